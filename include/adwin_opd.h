@@ -403,6 +403,122 @@ int adwin_opd_fused_profile(const adwin_opd_problem* p, void* workspace, size_t 
 int adwin_opd_from_logits_profile(const adwin_opd_logits_problem* p, void* workspace,
                                   size_t workspace_bytes, void* hip_stream, float* phase_ms);
 
+/* ---------------------------------------------------------------------------------------
+ * Scoring given tokens under ONE model: a head that is kept in 8-bit integers (the frozen
+ * teacher's, read but never trained), log-probabilities of given tokens with entropy and top
+ * alternatives, and the gradient of a loss on them.  The conventions above hold, except that
+ * rows may lie any number of entries apart (`ld_*` >= the row's length) and that x, h, z and
+ * dz need no more than the alignment of their entries; rows whose addresses are multiples of 16 bytes are
+ * read and written 16 bytes at a time.  T (N) = 0 is a call that does nothing.
+ *
+ * Rows that cannot be computed are EXCLUDED, as in the calls above: zeros in every output (-1 in
+ * top_ids), never an inf or NaN, and a bit of `row_status`, which is one word per row here.
+ *
+ * ADWIN_E_SHAPE: a size out of the range given with its struct, or ld_* shorter than a row.
+ * ADWIN_E_MODE: an unknown *_dtype, a temperature that is not a positive normal number, or a
+ * struct_bytes mismatch.
+ * --------------------------------------------------------------------------------------- */
+
+/* Entries of a row of 8-bit integers: H rounded up to whole 128-byte lines; those beyond H are zero. */
+#define ADWIN_QUANT_PITCH(H) (((H) + 127) / 128 * 128)
+/* longest row of 8-bit integers: sums of products of two of them stay within 32 bits          */
+#define ADWIN_QUANT_MAX_H 65536
+#define ADWIN_MAX_GIVEN 128   /* most given tokens per row                                     */
+#define ADWIN_MAX_TOP   64    /* most alternatives per row                                     */
+
+/* Rows to 8-bit integers with one scale per row: with a = max_j |x_j|,
+ *   scale = a / 127,   q_j = 127 x_j / a to the nearest integer, ties to the even one,
+ * so that x_j is scale q_j to half a step.  A row of zeros has scale 0.  A row with an inf or NaN is excluded:
+ * scale 0, q 0, ADWIN_DEV_NONFINITE in row_status.  Limits: 0 <= N < 2^31, 1 <= H <= ADWIN_QUANT_MAX_H. */
+typedef struct adwin_opd_quant_problem {
+  size_t  struct_bytes;      /* sizeof(adwin_opd_quant_problem), checked                       */
+  int64_t N;                 /* rows                                                           */
+  int64_t ld_x;              /* entries from one row of x to the next                          */
+  int32_t H, x_dtype;        /* entries of a row; ADWIN_DT_*                                   */
+  const void* x;             /* device [N, H]                                                  */
+  int8_t* q;                 /* device [N, ADWIN_QUANT_PITCH(H)], 16-byte aligned              */
+  float*  scale;             /* device [N]                                                     */
+  int32_t* row_status;       /* device [N], NULL = not wanted                                  */
+} adwin_opd_quant_problem;
+int adwin_opd_quant_rows(const adwin_opd_quant_problem* p, void* hip_stream);
+
+/* Logits of hidden states under a head kept in 8-bit integers: the rows of h are brought to 8 bits as
+ * above (q_h, s_h; in the workspace) and
+ *   z[t, v] = s_h[t] W_scale[v] sum_k q_h[t, k] W_q[v, k],
+ * the sum exact in 32-bit integers, one rounding of it to fp32 and one of z to its type.  The head is
+ * adwin_opd_quant_rows of W [V, H]: laid out once, or whenever the weights change.
+ * Limits: 0 <= T < 2^31, 1 <= V <= 2^28, 1 <= H <= ADWIN_QUANT_MAX_H. */
+typedef struct adwin_opd_quant_logits_problem {
+  size_t  struct_bytes;
+  int64_t T;
+  int64_t ld_h, ld_z;        /* entries from one row to the next                               */
+  int32_t V, H;
+  int32_t h_dtype, z_dtype;  /* ADWIN_DT_*                                                     */
+  const void*   h;           /* device [T, H]                                                  */
+  const int8_t* W_q;         /* device [V, ADWIN_QUANT_PITCH(H)], 16-byte aligned              */
+  const float*  W_scale;     /* device [V]                                                     */
+  void*    z;                /* device [T, V]                                                  */
+  int32_t* row_status;       /* device [T], NULL = not wanted: ADWIN_DEV_NONFINITE where h holds an inf or NaN (z is 0 there) */
+} adwin_opd_quant_logits_problem;
+int adwin_opd_quant_logits_workspace_bytes(const adwin_opd_quant_logits_problem* p, size_t* bytes);
+int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, void* workspace, size_t workspace_bytes,
+                           void* hip_stream);
+
+/* Log-probabilities of given tokens from logits z, at x = z / temperature:
+ *   m = max_j z_j,  s = sum_j exp((z_j - m) / temperature),
+ *   logp[g] = (z[ids[g]] - m) / temperature - log s,   entropy = -sum_j p_j log p_j,
+ *   top_ids / top_logp: the `top` largest logits in falling order, equal ones by rising index
+ *   (beyond V of them: -1 and 0).
+ * z may hold -inf (a masked entry: probability 0, it takes no part in the entropy; its
+ * log-probability is -inf where it is asked for).  An id < 0 is not scored (logp 0); an id >= V is not either and sets
+ * ADWIN_DEV_BAD_ID.  A row of which no id is scored is not read: zeros, -1 in top_ids (rows outside a window
+ * are given so).  With G = 0 every row is computed.  A row with a NaN or +inf, or of nothing but -inf,
+ * is excluded with ADWIN_DEV_NONFINITE.
+ * Limits: 0 <= T < 2^31, 1 <= V <= 2^28, 0 <= G <= ADWIN_MAX_GIVEN, 0 <= top <= ADWIN_MAX_TOP. */
+typedef struct adwin_opd_logp_problem {
+  size_t  struct_bytes;
+  int64_t T;
+  int64_t ld_z;
+  int32_t V, G, top;
+  int32_t z_dtype;           /* ADWIN_DT_*                                                     */
+  float   temperature;
+  const void*    z;          /* device [T, V]                                                  */
+  const int32_t* ids;        /* device [T, G]; NULL when G = 0                                 */
+  /* device outputs; NULL = not wanted */
+  float*   logp;             /* [T, G]                                                         */
+  float*   entropy;          /* [T]                                                            */
+  float*   norm;             /* [T, 2] m and s: what the gradient needs of this call; 0, 0 where excluded or not read */
+  int32_t* top_ids;          /* [T, top]                                                       */
+  float*   top_logp;         /* [T, top]                                                       */
+  int32_t* row_status;       /* [T] ADWIN_DEV_* bits                                           */
+} adwin_opd_logp_problem;
+int adwin_opd_token_logp_workspace_bytes(const adwin_opd_logp_problem* p, size_t* bytes);
+int adwin_opd_token_logp(const adwin_opd_logp_problem* p, void* workspace, size_t workspace_bytes,
+                         void* hip_stream);
+
+/* The gradient of a loss whose derivatives by logp and entropy are g_logp and g_entropy:
+ *   dz_j = ( sum_g g_logp[g] ([j = ids[g]] - p_j)  -  g_entropy p_j (log p_j + entropy) ) / temperature
+ * with p from norm, and norm and entropy as adwin_opd_token_logp wrote them for the same z, ids and
+ * temperature.  An id that a row names twice adds twice; what is not scored adds nothing.  Rows that are excluded
+ * or of which nothing is scored get zeros (G = 0: every row is computed).  For the alternatives' log-probabilities,
+ * or any other sparse loss, the tokens are given as ids.  dz may be z itself where types and pitches are equal. */
+typedef struct adwin_opd_logp_grad_problem {
+  size_t  struct_bytes;
+  int64_t T;
+  int64_t ld_z, ld_dz;
+  int32_t V, G;
+  int32_t z_dtype, dz_dtype; /* ADWIN_DT_*                                                     */
+  float   temperature;
+  const void*    z;          /* device [T, V]                                                  */
+  const int32_t* ids;        /* device [T, G]; NULL when G = 0                                 */
+  const float*   norm;       /* device [T, 2]                                                  */
+  const float*   g_logp;     /* device [T, G]; NULL when G = 0                                 */
+  const float*   entropy;    /* device [T]; NULL when g_entropy is                             */
+  const float*   g_entropy;  /* device [T], NULL = zeros                                       */
+  void*          dz;         /* device [T, V]                                                  */
+} adwin_opd_logp_grad_problem;
+int adwin_opd_token_logp_grad(const adwin_opd_logp_grad_problem* p, void* hip_stream);
+
 /*
  * Measured ceilings of the machine, for quoting roofline fractions against what the box
  * delivers as well as against the published peaks.  Both synchronise.

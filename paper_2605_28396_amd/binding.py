@@ -9,6 +9,7 @@ The function names are those of include/adwin_opd.h.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -30,6 +31,11 @@ ADWIN_STATIC_SCRATCH_BYTES = 1 << 20
 ADWIN_EST_EXPECTED, ADWIN_EST_SAMPLED = 0, 1
 ADWIN_SCHEME_AUTO, ADWIN_SCHEME_SINGLE, ADWIN_SCHEME_TWO_SWEEP, ADWIN_SCHEME_TWO_SWEEP_REG = 0, 1, 2, 3
 ADWIN_LOGITS_AUTO, ADWIN_LOGITS_RESIDENT, ADWIN_LOGITS_STREAMING = 0, 1, 2
+ADWIN_QUANT_MAX_H, ADWIN_MAX_GIVEN, ADWIN_MAX_TOP = 65536, 128, 64
+
+
+def ADWIN_QUANT_PITCH(H: int) -> int:
+    return (H + 127) // 128 * 128
 
 
 class adwin_opd_problem(C.Structure):
@@ -72,6 +78,40 @@ class adwin_opd_logits_problem(C.Structure):
     ]
 
 
+class adwin_opd_quant_problem(C.Structure):
+    _fields_ = [
+        ("struct_bytes", C.c_size_t), ("N", C.c_int64), ("ld_x", C.c_int64), ("H", C.c_int32), ("x_dtype", C.c_int32),
+        ("x", C.c_void_p), ("q", C.c_void_p), ("scale", C.c_void_p), ("row_status", C.c_void_p),
+    ]
+
+
+class adwin_opd_quant_logits_problem(C.Structure):
+    _fields_ = [
+        ("struct_bytes", C.c_size_t), ("T", C.c_int64), ("ld_h", C.c_int64), ("ld_z", C.c_int64),
+        ("V", C.c_int32), ("H", C.c_int32), ("h_dtype", C.c_int32), ("z_dtype", C.c_int32),
+        ("h", C.c_void_p), ("W_q", C.c_void_p), ("W_scale", C.c_void_p), ("z", C.c_void_p), ("row_status", C.c_void_p),
+    ]
+
+
+class adwin_opd_logp_problem(C.Structure):
+    _fields_ = [
+        ("struct_bytes", C.c_size_t), ("T", C.c_int64), ("ld_z", C.c_int64),
+        ("V", C.c_int32), ("G", C.c_int32), ("top", C.c_int32), ("z_dtype", C.c_int32), ("temperature", C.c_float),
+        ("z", C.c_void_p), ("ids", C.c_void_p),
+        ("logp", C.c_void_p), ("entropy", C.c_void_p), ("norm", C.c_void_p), ("top_ids", C.c_void_p),
+        ("top_logp", C.c_void_p), ("row_status", C.c_void_p),
+    ]
+
+
+class adwin_opd_logp_grad_problem(C.Structure):
+    _fields_ = [
+        ("struct_bytes", C.c_size_t), ("T", C.c_int64), ("ld_z", C.c_int64), ("ld_dz", C.c_int64),
+        ("V", C.c_int32), ("G", C.c_int32), ("z_dtype", C.c_int32), ("dz_dtype", C.c_int32), ("temperature", C.c_float),
+        ("z", C.c_void_p), ("ids", C.c_void_p), ("norm", C.c_void_p), ("g_logp", C.c_void_p), ("entropy", C.c_void_p),
+        ("g_entropy", C.c_void_p), ("dz", C.c_void_p),
+    ]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -111,6 +151,15 @@ def _load() -> C.CDLL:
     lib.adwin_opd_from_logits_profile.restype = C.c_int
     lib.adwin_opd_from_logits_profile.argtypes = [C.POINTER(adwin_opd_logits_problem), C.c_void_p,
                                                   C.c_size_t, C.c_void_p, C.POINTER(C.c_float)]
+    lib.adwin_opd_quant_rows.restype = C.c_int
+    lib.adwin_opd_quant_rows.argtypes = [C.POINTER(adwin_opd_quant_problem), C.c_void_p]
+    for name, problem in (("quant_logits", adwin_opd_quant_logits_problem), ("token_logp", adwin_opd_logp_problem)):
+        need, call = getattr(lib, f"adwin_opd_{name}_workspace_bytes"), getattr(lib, f"adwin_opd_{name}")
+        need.restype = call.restype = C.c_int
+        need.argtypes = [C.POINTER(problem), C.POINTER(C.c_size_t)]
+        call.argtypes = [C.POINTER(problem), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.adwin_opd_token_logp_grad.restype = C.c_int
+    lib.adwin_opd_token_logp_grad.argtypes = [C.POINTER(adwin_opd_logp_grad_problem), C.c_void_p]
     lib.adwin_opd_init.restype = C.c_int
     lib.adwin_opd_init.argtypes = []
     lib.adwin_opd_ceiling_copy.restype = C.c_int
@@ -406,6 +455,176 @@ def adwin_opd_from_logits_static(z_s, z_t, ids, offsets, window, stream=None, **
     call = LogitsCall(z_s, z_t, ids, offsets, window, workspace=False, **kw)
     _check(call.run_static(stream))
     return call.out
+
+
+# ---- scoring given tokens under one model ---------------------------------------------------------------------------
+
+_DTYPE = {torch.bfloat16: ADWIN_DT_BF16, torch.float32: ADWIN_DT_F32}
+_TORCH_DTYPE = (torch.bfloat16, torch.float32)
+
+
+def _on_stream(call):
+    """`stream`: where the call's work goes, and what its outputs and workspace are allocated on (default: the current
+    stream, which has to be the one that the inputs are ready on)."""
+    @functools.wraps(call)
+    def on(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+            return call(*args, **kw)
+    return on
+
+
+def _rows(name, x):
+    """The pitch of a 2-D array as the library takes it: on the GPU, whole rows of bf16 or fp32, any distance apart."""
+    if x.dim() != 2 or x.dtype not in _DTYPE or (x.stride(1) != 1 and x.shape[1] > 1) or not x.is_cuda:
+        raise ValueError(f"{name}: rows of contiguous entries of {', '.join(str(d) for d in _DTYPE)} on the GPU are taken, "
+                         f"not {tuple(x.shape)} of {x.dtype} with strides {x.stride()} on {x.device}")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+
+
+def _flat(name, x, dtype, *shape):
+    if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name}: a contiguous {shape} of {dtype} on the GPU is taken, not {tuple(x.shape)} of {x.dtype} with "
+                         f"strides {x.stride()} on {x.device}")
+    return x.data_ptr()
+
+
+@_on_stream
+def adwin_opd_quant_rows(x, row_status=False) -> dict:
+    """Rows x [N, H] (bf16, fp32) as 8-bit integers: `q` [N, ADWIN_QUANT_PITCH(H)], `scale` [N]."""
+    ld = _rows("x", x)
+    N, H = x.shape
+    q = torch.empty(N, ADWIN_QUANT_PITCH(H), dtype=torch.int8, device=x.device)
+    scale = torch.empty(N, dtype=torch.float32, device=x.device)
+    out = {"q": q, "scale": scale}
+    if row_status:
+        out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
+    p = adwin_opd_quant_problem(C.sizeof(adwin_opd_quant_problem), N, ld, H, _DTYPE[x.dtype], x.data_ptr(), q.data_ptr(),
+                                scale.data_ptr(), _ptr(out.get("row_status")))
+    _check(lib.adwin_opd_quant_rows(p, _stream_handle(None)))
+    return out
+
+
+def adwin_opd_quant_logits_workspace_bytes(p: adwin_opd_quant_logits_problem) -> int:
+    n = C.c_size_t(0)
+    _check(lib.adwin_opd_quant_logits_workspace_bytes(C.byref(p), C.byref(n)))
+    return int(n.value)
+
+
+@_on_stream
+def adwin_opd_quant_logits(h, W_q, W_scale, z_dtype=ADWIN_DT_BF16, z=None, row_status=False) -> dict:
+    """Logits `z` [T, V] of hidden states h [T, H] under the head that adwin_opd_quant_rows made of W [V, H].  z: where
+    they go (else a new tensor)."""
+    ld = _rows("h", h)
+    T, H = h.shape
+    V = W_q.shape[0]
+    W_ptr = _flat("W_q", W_q, torch.int8, V, ADWIN_QUANT_PITCH(H))
+    s_ptr = _flat("W_scale", W_scale, torch.float32, V)
+    if z is None:
+        z = torch.empty(T, V, dtype=_TORCH_DTYPE[z_dtype], device=h.device)
+        ld_z = V
+    else:
+        ld_z = _rows("z", z)
+        z_dtype = _DTYPE[z.dtype]
+        if tuple(z.shape) != (T, V):
+            raise ValueError(f"z: {(T, V)} is taken, not {tuple(z.shape)}")
+    out = {"z": z}
+    if row_status:
+        out["row_status"] = torch.empty(T, dtype=torch.int32, device=h.device)
+    p = adwin_opd_quant_logits_problem(C.sizeof(adwin_opd_quant_logits_problem), T, ld, ld_z, V, H, _DTYPE[h.dtype], z_dtype,
+                                       h.data_ptr(), W_ptr, s_ptr, z.data_ptr(), _ptr(out.get("row_status")))
+    need = adwin_opd_quant_logits_workspace_bytes(p)
+    ws = torch.empty(need, dtype=torch.uint8, device=h.device)
+    _check(lib.adwin_opd_quant_logits(p, ws.data_ptr(), need, _stream_handle(None)))
+    return out
+
+
+class QuantHead:
+    """A head W [V, H] kept in 8-bit integers; set(W) lays it out again after its weights have changed."""
+
+    def __init__(self, W, stream=None):
+        self.set(W, stream)
+
+    def set(self, W, stream=None):
+        out = adwin_opd_quant_rows(W, stream=stream)
+        self.W_q, self.W_scale, self.H = out["q"], out["scale"], int(W.shape[1])
+
+    def logits(self, h, z_dtype=ADWIN_DT_BF16, z=None, stream=None):
+        return adwin_opd_quant_logits(h, self.W_q, self.W_scale, z_dtype=z_dtype, z=z, stream=stream)["z"]
+
+
+def adwin_opd_token_logp_workspace_bytes(p: adwin_opd_logp_problem) -> int:
+    n = C.c_size_t(0)
+    _check(lib.adwin_opd_token_logp_workspace_bytes(C.byref(p), C.byref(n)))
+    return int(n.value)
+
+
+def _given(ids, T):
+    """(G, pointer) of the ids of a call; [T] is one per row."""
+    if ids is None:
+        return 0, None
+    G = 1 if ids.dim() == 1 else int(ids.shape[1])
+    return G, _flat("ids", ids, torch.int32, *((T,) if ids.dim() == 1 else (T, G)))
+
+
+@_on_stream
+def adwin_opd_token_logp(z, ids=None, temperature=1.0, top=0, row_status=False) -> dict:
+    """Of logits z [T, V] (bf16, fp32): `logp` of the tokens ids [T, G] (or [T]; int32, negative: not scored), `entropy`,
+    the `top` largest as `top_ids`, `top_logp`, and `norm`, which adwin_opd_token_logp_grad takes."""
+    ld = _rows("z", z)
+    T, V = z.shape
+    G, ids_ptr = _given(ids, T)
+    dev, f32 = z.device, torch.float32
+    entropy = torch.empty(T, dtype=f32, device=dev)
+    norm = torch.empty(T, 2, dtype=f32, device=dev)
+    out = {"entropy": entropy, "norm": norm}
+    if G:
+        out["logp"] = torch.empty(T, G, dtype=f32, device=dev) if ids.dim() == 2 else torch.empty(T, dtype=f32, device=dev)
+    if top:
+        out["top_ids"] = torch.empty(T, top, dtype=torch.int32, device=dev)
+        out["top_logp"] = torch.empty(T, top, dtype=f32, device=dev)
+    if row_status:
+        out["row_status"] = torch.empty(T, dtype=torch.int32, device=dev)
+    p = adwin_opd_logp_problem(C.sizeof(adwin_opd_logp_problem), T, ld, V, G, top, _DTYPE[z.dtype], temperature,
+                               z.data_ptr(), ids_ptr, _ptr(out.get("logp")), entropy.data_ptr(), norm.data_ptr(),
+                               _ptr(out.get("top_ids")), _ptr(out.get("top_logp")), _ptr(out.get("row_status")))
+    need = adwin_opd_token_logp_workspace_bytes(p)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _check(lib.adwin_opd_token_logp(p, _ptr(ws), need, _stream_handle(None)))
+    return out
+
+
+@_on_stream
+def adwin_opd_token_logp_grad(z, ids, norm, g_logp, entropy=None, g_entropy=None, temperature=1.0, dz_dtype=None,
+                              dz=None) -> dict:
+    """Gradient `dz` [T, V] of a loss with the derivatives g_logp [T, G] and g_entropy [T] by the outputs of
+    adwin_opd_token_logp on the same z, ids and temperature.  dz: where it goes (z itself is allowed); else a new tensor
+    of dz_dtype, or of z's."""
+    ld = _rows("z", z)
+    T, V = z.shape
+    G, ids_ptr = _given(ids, T)
+    f32 = torch.float32
+    norm_ptr = _flat("norm", norm, f32, T, 2)
+    g_ptr = _flat("g_logp", g_logp, f32, *ids.shape) if G else None
+    ge_ptr = h_ptr = None
+    if g_entropy is not None:
+        if entropy is None:
+            raise ValueError("g_entropy needs entropy")
+        ge_ptr, h_ptr = _flat("g_entropy", g_entropy, f32, T), _flat("entropy", entropy, f32, T)
+    if dz is None:
+        dz_dtype = _DTYPE[z.dtype] if dz_dtype is None else dz_dtype
+        dz = torch.empty(T, V, dtype=_TORCH_DTYPE[dz_dtype], device=z.device)
+        ld_dz = V
+    else:
+        ld_dz = _rows("dz", dz)
+        dz_dtype = _DTYPE[dz.dtype]
+        if tuple(dz.shape) != (T, V):
+            raise ValueError(f"dz: {(T, V)} is taken, not {tuple(dz.shape)}")
+    p = adwin_opd_logp_grad_problem(C.sizeof(adwin_opd_logp_grad_problem), T, ld, ld_dz, V, G, _DTYPE[z.dtype], dz_dtype,
+                                    temperature, z.data_ptr(), ids_ptr, norm_ptr, g_ptr, h_ptr, ge_ptr, dz.data_ptr())
+    _check(lib.adwin_opd_token_logp_grad(p, _stream_handle(None)))
+    return {"dz": dz}
 
 
 def adwin_opd_init() -> None:

@@ -1,0 +1,392 @@
+// Log-probabilities of given tokens with entropy and top alternatives, and their gradient.
+//
+// With x_j = z_j / temperature, m = max z, s = sum_j exp((z_j - m) / temperature):
+//   log p_j = (z_j - m) / temperature - log s,   H = log s - (1/s) sum_j e_j (z_j - m) / temperature.
+// Exponentials are taken to the base 2: d_j = c z_j - r with c = log2(e) / temperature and a thread's own reference r,
+// one fp32 number that is subtracted inside one fma and added back in one, so that its rounding is no error.
+#include "score_shared.h"
+
+namespace adwin {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+struct LogpArgs {
+  const void* z; int64_t ld; int64_t T;
+  int32_t V, G, top;
+  float temperature, c;             // c = log2(e) / temperature
+  const int32_t* ids;
+  float* logp; float* entropy; float* norm; int32_t* top_ids; float* top_logp; int32_t* row_status;
+};
+
+// ---- order of the alternatives --------------------------------------------------------
+// One 64-bit word per entry, larger for the larger logit and then for the lower index (-0 counts as 0).
+__device__ __forceinline__ uint32_t order_bits(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint64_t order_key(float x, int i) {
+  return ((uint64_t)order_bits(x) << 32) | (uint32_t)~i;
+}
+__device__ __forceinline__ int key_index(uint64_t k) { return ~(int)(uint32_t)k; }
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t b = (uint32_t)(k >> 32);
+  return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+
+// Running sums of one thread, relative to its reference r (in units of the exponent to the base 2).
+struct Sums { float r, s, t, m; };      // s = sum 2^d, t = sum 2^d d, m = largest logit
+constexpr float kNoRef = -1.0e38f;
+constexpr float kSlack = 16.f;          // d may reach this before the reference moves: 2^16 a term is far from the end of fp32
+__device__ __forceinline__ Sums no_sums() { return {kNoRef, 0.f, 0.f, -INFINITY}; }
+
+__device__ __forceinline__ void add_one(Sums& a, float z, float c) {
+  const float d = fmaf(z, c, -a.r), e = fast_exp2(d);
+  a.s += e;
+  a.t = fmaf(e, fmaxf(d, kNegBig), a.t);     // a masked entry is 0 times something finite
+}
+__device__ __forceinline__ void move_ref(Sums& a, float r) {
+  const float by = a.r - r, f = fast_exp2(by);
+  a.t = f * fmaf(a.s, fmaxf(by, kNegBig), a.t);
+  a.s *= f;
+  a.r = r;
+}
+template <int N>
+__device__ __forceinline__ void add_entries(Sums& a, const float (&x)[N], float c) {
+  float m = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+  a.m = fmaxf(a.m, m);
+  if (m * c > a.r + kSlack) move_ref(a, m * c);
+#pragma unroll
+  for (int i = 0; i < N; ++i) add_one(a, x[i], c);
+}
+__device__ __forceinline__ void merge_sums(Sums& a, Sums b) {
+  if (b.r > a.r) { const Sums x = a; a = b; b = x; }
+  move_ref(b, a.r);
+  a.s += b.s;
+  a.t += b.t;
+  a.m = fmaxf(a.m, b.m);
+}
+
+__device__ __forceinline__ Sums block_sums(Sums a, float (*part)[4]) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const Sums b = {__shfl_xor(a.r, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64), __shfl_xor(a.m, o, 64)};
+    merge_sums(a, b);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    float* q = part[threadIdx.x >> 6];
+    q[0] = a.r; q[1] = a.s; q[2] = a.t; q[3] = a.m;
+  }
+  __syncthreads();
+  a = {part[0][0], part[0][1], part[0][2], part[0][3]};
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) merge_sums(a, Sums{part[w][0], part[w][1], part[w][2], part[w][3]});
+  return a;
+}
+
+// The `top` largest keys of the row, sorted, in `kept`.  Round by round over 256 vectors: a thread's largest key is
+// ranked among the threads', the top-th of these is a bound that at most `top` threads pass, and what passes it and
+// the last of the kept ones is ranked together with those.  Exact for any input.
+template <typename T>
+__device__ void select_top(const RowSpan<T>& row, int top, uint64_t* kept, uint64_t* found, uint64_t* best, int* count) {
+  constexpr int N = Entry<T>::kPerVec;
+  const int tid = threadIdx.x;
+  int have = 0;
+  const int rounds = (row.vecs + kThreads - 1) / kThreads;
+  for (int k = -1; k < rounds; ++k) {             // the edge first
+    uint64_t key[N];
+    const int i = k * kThreads + tid;
+#pragma unroll
+    for (int e = 0; e < N; ++e) key[e] = 0;
+    if (k < 0) {
+      if (tid < row.edge) key[0] = order_key(Entry<T>::one(row.p + row.edge_index(tid)), row.edge_index(tid));
+    } else if (i < row.vecs) {
+      float x[N];
+      Entry<T>::unpack(row.vec(i), x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) key[e] = order_key(x[e], row.index(i) + e);
+    }
+    uint64_t mine = key[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) mine = key[e] > mine ? key[e] : mine;
+    best[tid] = mine;
+    if (tid == 0) { *count = 0; best[kThreads] = 0; }
+    __syncthreads();
+    int rank = 0;
+    for (int j = 0; j < kThreads; ++j) rank += best[j] > mine;
+    if (rank == top - 1 && mine) best[kThreads] = mine;      // keys differ, but for the zeros of idle threads
+    __syncthreads();
+    uint64_t bound = best[kThreads];
+    if (have == top && kept[top - 1] > bound) bound = kept[top - 1] + 1;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (key[e] && key[e] >= bound) found[atomicAdd(count, 1)] = key[e];
+    __syncthreads();
+    const int n = *count;                        // at most top threads times N
+    if (n) {
+      uint64_t keep[3] = {0, 0, 0};
+      int at[3];
+#pragma unroll
+      for (int u = 0; u < 3; ++u) {
+        const int q = u * kThreads + tid;
+        if (q < n + have) {
+          const uint64_t v = q < n ? found[q] : kept[q - n];
+          int r = 0;
+          for (int j = 0; j < n; ++j) r += found[j] > v;
+          for (int j = 0; j < have; ++j) r += kept[j] > v;
+          keep[u] = v; at[u] = r;
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < 3; ++u)
+        if (keep[u] && at[u] < top) kept[at[u]] = keep[u];
+      have = have + n < top ? have + n : top;
+    }
+    __syncthreads();
+  }
+  if (tid >= have && tid < top) kept[tid] = 0;
+  __syncthreads();
+}
+
+// The sums relative to the row's largest logit, which is what is put out: 1 <= s, and the entropy log s - t / s
+// has no terms larger than need be.  `far` rows are at the end of the type's range, where c z overflows: differences first.
+template <typename T>
+__device__ Sums row_sums(const RowSpan<T>& row, const Sums& mine, float c, float (*part)[4]) {
+  Sums a = block_sums(mine, part);
+  const bool far = fabsf(a.m * c) > 1.0e30f && fabsf(a.m) < INFINITY;
+  if (!far) {
+    const float by = -fmaf(a.m, c, -a.r), f = fast_exp2(by);
+    a.t = f * fmaf(a.s, by, a.t);
+    a.s *= f;
+    return a;
+  }
+  __syncthreads();
+  Sums b = {0.f, 0.f, 0.f, a.m};
+  for (int i = threadIdx.x; i < row.n; i += kThreads) {
+    const float d = (Entry<T>::one(row.p + i) - a.m) * c, e = fast_exp2(d);
+    b.s += e;
+    b.t = fmaf(e, fmaxf(d, kNegBig), b.t);
+  }
+  return block_sums(b, part);
+}
+
+// 1 where some id of the row is scored (or G = 0); every thread of the workgroup gets the answer
+__device__ __forceinline__ int row_is_scored(const int32_t* ids, int G, int V, int64_t row, int* bad) {
+  int id = -1;
+  if ((int)threadIdx.x < G) id = ids[row * G + threadIdx.x];
+  *bad = __syncthreads_or(id >= V);
+  return G == 0 ? 1 : __syncthreads_or(id >= 0 && id < V);
+}
+
+template <typename T>
+__device__ void finish_row(const LogpArgs& a, int64_t row, const Sums& sum, const uint64_t* kept, int live, int bad) {
+  const T* z = (const T*)a.z + row * a.ld;
+  const int tid = threadIdx.x;
+  const float s = sum.s;
+  const bool fine = live && s > 0.f && s < INFINITY && fabsf(sum.m) < INFINITY;
+  const float ls = fine ? logf(s) : 0.f;
+  if (tid < a.G && a.logp) {
+    const int id = a.ids[row * a.G + tid];
+    float v = 0.f;
+    if (fine && id >= 0 && id < a.V) v = (Entry<T>::one(z + id) - sum.m) / a.temperature - ls;
+    a.logp[row * a.G + tid] = v;
+  }
+  if (tid < a.top) {
+    const uint64_t k = kept[tid];
+    const bool is = fine && k;
+    if (a.top_ids) a.top_ids[row * a.top + tid] = is ? key_index(k) : -1;
+    if (a.top_logp) a.top_logp[row * a.top + tid] = is ? (key_value(k) - sum.m) / a.temperature - ls : 0.f;
+  }
+  if (tid == 0) {
+    if (a.entropy) a.entropy[row] = fine ? fmaxf(0.f, fmaf(-kLn2, sum.t / s, ls)) : 0.f;
+    if (a.norm) { a.norm[2 * row] = fine ? sum.m : 0.f; a.norm[2 * row + 1] = fine ? s : 0.f; }
+    if (a.row_status) a.row_status[row] = (bad ? ADWIN_DEV_BAD_ID : 0) | (live && !fine ? ADWIN_DEV_NONFINITE : 0);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void token_logp_kernel(LogpArgs a) {
+  constexpr int N = Entry<T>::kPerVec;
+  __shared__ uint64_t kept[ADWIN_MAX_TOP], found[ADWIN_MAX_TOP * 8], best[kThreads + 1];
+  __shared__ float part[kWaves][4];
+  __shared__ int count;
+  const int64_t r = blockIdx.x;
+  int bad;
+  const int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
+  Sums sum = no_sums();
+  if (live) {
+    const RowSpan<T> row((const T*)a.z + r * a.ld, a.V);
+    if ((int)threadIdx.x < row.edge) {
+      const float x[1] = {Entry<T>::one(row.p + row.edge_index(threadIdx.x))};
+      add_entries(sum, x, a.c);
+    }
+    for (int i = threadIdx.x; i < row.vecs; i += kThreads) {
+      float x[N];
+      Entry<T>::unpack(row.vec(i), x);
+      add_entries(sum, x, a.c);
+    }
+    sum = row_sums<T>(row, sum, a.c, part);
+    if (a.top > 0) select_top<T>(row, a.top, kept, found, best, &count);
+  }
+  finish_row<T>(a, r, sum, kept, live, bad);
+}
+
+// ---------------------------------------------------------------------------------------
+// dz_j = -p_j (a + g_H (log p_j + H)) / temperature, a = sum_g g_g, and g_g / temperature more at the given tokens, whose
+// entries are computed again and written once more after the row (they were read before it: dz may be z).
+// ---------------------------------------------------------------------------------------
+struct LogpGradArgs {
+  const void* z; int64_t ld_z; void* dz; int64_t ld_dz; int64_t T;
+  int32_t V, G;
+  float c, per_temperature;
+  const int32_t* ids; const float* norm; const float* g_logp; const float* entropy; const float* g_entropy;
+};
+
+struct GradRow {
+  float m, c, per_s, log_s, a, gh, H, per_temperature;
+  __device__ __forceinline__ float plain(float z) const {       // times temperature
+    const float d = fmaxf((z - m) * c, kNegBig);
+    const float p = fast_exp2(d) * per_s;
+    return -p * fmaf(gh, fmaf(d, kLn2, H - log_s), a);
+  }
+};
+
+template <typename TI, typename TO>
+__global__ __launch_bounds__(kThreads) void token_logp_grad_kernel(LogpGradArgs a) {
+  constexpr int N = Entry<TI>::kPerVec;
+  __shared__ float at_id[ADWIN_MAX_GIVEN], g_of[ADWIN_MAX_GIVEN];
+  __shared__ int id_of[ADWIN_MAX_GIVEN];
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x;
+  int bad;
+  int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
+  const float s = live ? a.norm[2 * r + 1] : 0.f;
+  live = live && s > 0.f;
+  TO* out = (TO*)a.dz + r * a.ld_dz;
+  const RowSpan<TI> row((const TI*)a.z + r * a.ld_z, a.V);
+  GradRow g{};
+  if (live) {
+    if (tid < a.G) {
+      const int id = a.ids[r * a.G + tid];
+      const bool in = id >= 0 && id < a.V;
+      id_of[tid] = in ? id : -1;
+      g_of[tid] = in ? a.g_logp[r * a.G + tid] : 0.f;
+      at_id[tid] = in ? Entry<TI>::one(row.p + id) : 0.f;
+    }
+    __syncthreads();
+    g.m = a.norm[2 * r]; g.c = a.c; g.per_s = 1.f / s; g.log_s = logf(s); g.per_temperature = a.per_temperature;
+    g.gh = a.g_entropy ? a.g_entropy[r] : 0.f;
+    g.H = a.g_entropy ? a.entropy[r] : 0.f;
+    for (int j = 0; j < a.G; ++j) g.a += g_of[j];
+  }
+  if (tid < row.edge) {
+    const int i = row.edge_index(tid);
+    Entry<TO>::put(out + i, live ? g.plain(Entry<TI>::one(row.p + i)) * g.per_temperature : 0.f);
+  }
+  const bool aligned = ((uintptr_t)(out + row.head) & 15) == 0;
+  for (int i = tid; i < row.vecs; i += kThreads) {
+    float y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = 0.f;
+    if (live) {
+      float x[N];
+      Entry<TI>::unpack(row.vec(i), x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[e] = g.plain(x[e]) * g.per_temperature;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) Entry<TO>::put(out + row.index(i) + e, y[e]);
+  }
+  (void)aligned;
+  if (!live) return;
+  __syncthreads();                               // the row's stores come before those of the given tokens
+  if (tid < a.G && id_of[tid] >= 0) {
+    const int id = id_of[tid];
+    bool first = true;
+    for (int j = 0; j < tid; ++j) first = first && id_of[j] != id;
+    if (first) {
+      float sum = 0.f;
+      for (int j = tid; j < a.G; ++j) sum += id_of[j] == id ? g_of[j] : 0.f;
+      Entry<TO>::put(out + id, (sum + g.plain(at_id[tid])) * g.per_temperature);
+    }
+  }
+}
+
+static bool known_temperature(float t) { return t >= 1.17549435e-38f && t <= 3.0e38f; }
+
+static int check_logp(const adwin_opd_logp_problem* p) {
+  if (!p) return ADWIN_E_NULL;
+  if (p->struct_bytes != sizeof(*p) || !known_dtype(p->z_dtype) || !known_temperature(p->temperature)) return ADWIN_E_MODE;
+  if (p->T < 0 || p->T >= kMaxRows || p->V < 1 || p->V > kMaxVocab || p->ld_z < p->V || p->G < 0 || p->G > ADWIN_MAX_GIVEN ||
+      p->top < 0 || p->top > ADWIN_MAX_TOP)
+    return ADWIN_E_SHAPE;
+  return ADWIN_OK;
+}
+
+static int check_logp_grad(const adwin_opd_logp_grad_problem* p) {
+  if (!p) return ADWIN_E_NULL;
+  if (p->struct_bytes != sizeof(*p) || !known_dtype(p->z_dtype) || !known_dtype(p->dz_dtype) ||
+      !known_temperature(p->temperature))
+    return ADWIN_E_MODE;
+  if (p->T < 0 || p->T >= kMaxRows || p->V < 1 || p->V > kMaxVocab || p->ld_z < p->V || p->ld_dz < p->V || p->G < 0 ||
+      p->G > ADWIN_MAX_GIVEN)
+    return ADWIN_E_SHAPE;
+  return ADWIN_OK;
+}
+
+}  // namespace adwin
+
+using namespace adwin;
+
+extern "C" int adwin_opd_token_logp_workspace_bytes(const adwin_opd_logp_problem* p, size_t* bytes) {
+  if (!bytes) return ADWIN_E_NULL;
+  const int st = check_logp(p);
+  if (st != ADWIN_OK) return st;
+  *bytes = 0;
+  return ADWIN_OK;
+}
+
+extern "C" int adwin_opd_token_logp(const adwin_opd_logp_problem* p, void* workspace, size_t workspace_bytes,
+                                    void* hip_stream) {
+  const int st = check_logp(p);
+  if (st != ADWIN_OK) return st;
+  if (p->T == 0) return ADWIN_OK;
+  if (!p->z || (p->G > 0 && !p->ids)) return ADWIN_E_NULL;
+  if ((uintptr_t)p->z & entry_mask(p->z_dtype)) return ADWIN_E_ALIGN;
+  LogpArgs a{};
+  a.z = p->z; a.ld = p->ld_z; a.T = p->T; a.V = p->V; a.G = p->G; a.top = p->top;
+  a.temperature = p->temperature; a.c = (float)(1.4426950408889634 / (double)p->temperature);
+  a.ids = p->ids; a.logp = p->logp; a.entropy = p->entropy; a.norm = p->norm; a.top_ids = p->top_ids;
+  a.top_logp = p->top_logp; a.row_status = p->row_status;
+  if (!a.top_ids && !a.top_logp) a.top = 0;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  if (p->z_dtype == ADWIN_DT_BF16) token_logp_kernel<uint16_t><<<(unsigned)p->T, kThreads, 0, stream>>>(a);
+  else token_logp_kernel<float><<<(unsigned)p->T, kThreads, 0, stream>>>(a);
+  ADWIN_HIP_TRY(hipGetLastError());
+  return ADWIN_OK;
+}
+
+extern "C" int adwin_opd_token_logp_grad(const adwin_opd_logp_grad_problem* p, void* hip_stream) {
+  const int st = check_logp_grad(p);
+  if (st != ADWIN_OK) return st;
+  if (p->T == 0) return ADWIN_OK;
+  if (!p->z || !p->dz || !p->norm || (p->G > 0 && (!p->ids || !p->g_logp)) || (p->g_entropy && !p->entropy))
+    return ADWIN_E_NULL;
+  if (((uintptr_t)p->z & entry_mask(p->z_dtype)) || ((uintptr_t)p->dz & entry_mask(p->dz_dtype))) return ADWIN_E_ALIGN;
+  LogpGradArgs a{};
+  a.z = p->z; a.ld_z = p->ld_z; a.dz = p->dz; a.ld_dz = p->ld_dz; a.T = p->T; a.V = p->V; a.G = p->G;
+  a.c = (float)(1.4426950408889634 / (double)p->temperature); a.per_temperature = 1.f / p->temperature;
+  a.ids = p->ids; a.norm = p->norm; a.g_logp = p->g_logp; a.entropy = p->entropy; a.g_entropy = p->g_entropy;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  const bool in16 = p->z_dtype == ADWIN_DT_BF16, out16 = p->dz_dtype == ADWIN_DT_BF16;
+  const unsigned blocks = (unsigned)p->T;
+  if (in16 && out16) token_logp_grad_kernel<uint16_t, uint16_t><<<blocks, kThreads, 0, stream>>>(a);
+  else if (in16) token_logp_grad_kernel<uint16_t, float><<<blocks, kThreads, 0, stream>>>(a);
+  else if (out16) token_logp_grad_kernel<float, uint16_t><<<blocks, kThreads, 0, stream>>>(a);
+  else token_logp_grad_kernel<float, float><<<blocks, kThreads, 0, stream>>>(a);
+  ADWIN_HIP_TRY(hipGetLastError());
+  return ADWIN_OK;
+}

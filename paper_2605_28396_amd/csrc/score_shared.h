@@ -1,0 +1,59 @@
+// What the token-scoring kernels share: entries of bf16 or fp32, rows at any address.
+#pragma once
+#include "common.h"
+#include "device_utils.h"
+
+namespace adwin {
+
+// 16 bytes of a row: 8 entries of bf16, 4 of fp32.
+template <typename T> struct Entry;
+template <> struct Entry<uint16_t> {               // bf16
+  static constexpr int kPerVec = 8;
+  static __device__ __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  }
+  static __device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)pack_bf16(x, 0.f); }
+};
+template <> struct Entry<float> {
+  static constexpr int kPerVec = 4;
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
+};
+
+// A row of n entries at any address that suits its entries: `head` entries up to the first multiple of 16 bytes,
+// `vecs` whole vectors behind them, and `edge` entries outside the vectors (the head's and those after the last vector).
+template <typename T>
+struct RowSpan {
+  static constexpr int kPer = Entry<T>::kPerVec;
+  const T* p;
+  int n, head, vecs, edge;
+  __device__ __forceinline__ RowSpan(const T* row, int entries) : p(row), n(entries) {
+    const int over = (int)((uintptr_t)row & 15) / (int)sizeof(T);
+    head = over ? kPer - over : 0;
+    if (head > n) head = n;
+    vecs = (n - head) / kPer;
+    edge = n - vecs * kPer;
+  }
+  __device__ __forceinline__ int edge_index(int e) const { return e < head ? e : e + vecs * kPer; }
+  __device__ __forceinline__ uint4 vec(int i) const { return ((const uint4*)(p + head))[i]; }
+  __device__ __forceinline__ int index(int i) const { return head + i * kPer; }
+};
+
+inline bool known_dtype(int32_t d) { return d == ADWIN_DT_BF16 || d == ADWIN_DT_F32; }
+inline uintptr_t entry_mask(int32_t d) { return d == ADWIN_DT_BF16 ? 1 : 3; }
+constexpr int64_t kMaxRows = (int64_t)1 << 31;      // rows of a call: fewer than this
+constexpr int32_t kMaxVocab = 1 << 28;
+
+}  // namespace adwin
