@@ -2,8 +2,7 @@
 //
 // With x_j = z_j / temperature, m = max z, s = sum_j exp((z_j - m) / temperature):
 //   log p_j = (z_j - m) / temperature - log s,   H = log s - (1/s) sum_j e_j (z_j - m) / temperature.
-// Exponentials are taken to the base 2: d_j = c z_j - r with c = log2(e) / temperature and a thread's own reference r,
-// one fp32 number that is subtracted inside one fma and added back in one, so that its rounding is no error.
+// Exponentials are taken to the base 2: d_j = c z_j - r, one fma, with c = log2(e) / temperature and a thread's own reference r.
 #include "score_shared.h"
 
 namespace adwin {
@@ -14,6 +13,9 @@ constexpr int kWaves = kThreads / 64;
 struct LogpArgs {
   const void* z; int64_t ld; int64_t T;
   int32_t V, G, top;
+  int32_t pieces;                   // workgroups per row; their sums and keys in `part`, `keys` where there are several
+  float* part;                      // [T][pieces][4] m, s, t, 0
+  uint64_t* keys;                   // [T][pieces][top]
   float temperature, c;             // c = log2(e) / temperature
   const int32_t* ids;
   float* logp; float* entropy; float* norm; int32_t* top_ids; float* top_logp; int32_t* row_status;
@@ -37,7 +39,12 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 // Running sums of one thread, relative to its reference r (in units of the exponent to the base 2).
 struct Sums { float r, s, t, m; };      // s = sum 2^d, t = sum 2^d d, m = largest logit
 constexpr float kNoRef = -1.0e38f;
-constexpr float kSlack = 16.f;          // d may reach this before the reference moves: 2^16 a term is far from the end of fp32
+// d may reach this before the reference moves.  Exponentials bear more (2^16 is far from the end of fp32), but the largest
+// term's d is rounded where it is summed into t and cancels only there: with 16 the entropy of a peaked row was off by 1e-6.
+constexpr float kSlack = 4.f;
+// References are whole numbers, so that moving and merging sums multiplies by exact powers of two (with the threads' largest
+// exponents themselves, the roundings of their differences were the same for all terms of a thread: s was off by 9e-7 where it is 1e-7 now).
+__device__ __forceinline__ float ref_of(float m, float c) { return ceilf(m * c); }
 __device__ __forceinline__ Sums no_sums() { return {kNoRef, 0.f, 0.f, -INFINITY}; }
 
 __device__ __forceinline__ void add_one(Sums& a, float z, float c) {
@@ -57,7 +64,7 @@ __device__ __forceinline__ void add_entries(Sums& a, const float (&x)[N], float 
 #pragma unroll
   for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
   a.m = fmaxf(a.m, m);
-  if (m * c > a.r + kSlack) move_ref(a, m * c);
+  if (m * c > a.r + kSlack) move_ref(a, ref_of(m, c));
 #pragma unroll
   for (int i = 0; i < N; ++i) add_one(a, x[i], c);
 }
@@ -86,77 +93,158 @@ __device__ __forceinline__ Sums block_sums(Sums a, float (*part)[4]) {
   return a;
 }
 
-// The `top` largest keys of the row, sorted, in `kept`.  Round by round over 256 vectors: a thread's largest key is
-// ranked among the threads', the top-th of these is a bound that at most `top` threads pass, and what passes it and
-// the last of the kept ones is ranked together with those.  Exact for any input.
+// Part of a row: vectors [v0, v1), and the row's edge entries with the first part.
 template <typename T>
-__device__ void select_top(const RowSpan<T>& row, int top, uint64_t* kept, uint64_t* found, uint64_t* best, int* count) {
+struct Piece {
+  RowSpan<T> row;
+  int v0, v1, edge;
+  __device__ __forceinline__ Piece(const T* p, int n, int piece, int pieces) : row(p, n) {
+    v0 = (int)((int64_t)row.vecs * piece / pieces);
+    v1 = (int)((int64_t)row.vecs * (piece + 1) / pieces);
+    edge = piece == 0 ? row.edge : 0;
+  }
+};
+
+constexpr int kFound = 1536;       // keys that a workgroup can list: 1,100 pass the first bound at top = 64 and V = 151,936
+
+struct Select {                    // in the LDS
+  uint64_t kept[ADWIN_MAX_TOP];    // the result: sorted, zeros behind the last
+  uint64_t found[kFound];
+  uint64_t best[kThreads + 1];
+  uint32_t most[kThreads];         // the threads' largest entries, as order_bits >> 16
+  int count, chosen;
+};
+
+// A lower bound of the `top`-th largest of the 256 numbers in `most`, exact in 16 bits, by every wave: the bits from the
+// highest on, a bit stays where at least `top` numbers reach it.  0 where fewer than `top` are above 0.
+__device__ __forceinline__ uint32_t wave_bound(const uint32_t* most, int top) {
+  const int lane = threadIdx.x & 63;
+  uint32_t v[kWaves];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) v[w] = most[64 * w + lane];
+  uint32_t at = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t t = at | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(v[w] >= t));
+    if (n >= top) at = t;
+  }
+  return at;
+}
+// the smallest logit whose order_bits reach at << 16
+__device__ __forceinline__ float bound_value(uint32_t at) {
+  if (at <= 0x007fu) return -INFINITY;              // order_bits(-inf) = 0x007fffff
+  const uint32_t b = at << 16;
+  return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+
+// found[0, n): the `top` largest of them into `kept`, by counting the larger ones.  Keys differ.
+__device__ __forceinline__ void rank_found(Select& l, int n, int top) {
+  for (int q = threadIdx.x; q < n; q += kThreads) {
+    const uint64_t v = l.found[q];
+    int r = 0;
+    for (int j = 0; j < n; ++j) r += l.found[j] > v;
+    if (r < top) l.kept[r] = v;
+  }
+  if ((int)threadIdx.x >= n && (int)threadIdx.x < top) l.kept[threadIdx.x] = 0;
+}
+
+// The `top` largest keys of a piece for any input, where more entries pass the bounds than can be listed (ties, rows in
+// rising order).  Round by round over 256 vectors: a thread's largest key is ranked among the threads', the
+// top-th of these is a bound that at most `top` threads pass, and what passes it and the last of the kept ones is ranked
+// together with those.
+template <typename T>
+__device__ __forceinline__ void select_slowly(const Piece<T>& p, int top, Select& l) {
   constexpr int N = Entry<T>::kPerVec;
   const int tid = threadIdx.x;
   int have = 0;
-  const int rounds = (row.vecs + kThreads - 1) / kThreads;
-  for (int k = -1; k < rounds; ++k) {             // the edge first
+  const int rounds = (p.v1 - p.v0 + kThreads - 1) / kThreads;
+  for (int k = p.edge ? -1 : 0; k < rounds; ++k) {             // the edge first
     uint64_t key[N];
-    const int i = k * kThreads + tid;
+    const int i = p.v0 + k * kThreads + tid;
 #pragma unroll
     for (int e = 0; e < N; ++e) key[e] = 0;
     if (k < 0) {
-      if (tid < row.edge) key[0] = order_key(Entry<T>::one(row.p + row.edge_index(tid)), row.edge_index(tid));
-    } else if (i < row.vecs) {
+      if (tid < p.edge) key[0] = order_key(Entry<T>::one(p.row.p + p.row.edge_index(tid)), p.row.edge_index(tid));
+    } else if (i < p.v1) {
       float x[N];
-      Entry<T>::unpack(row.vec(i), x);
+      Entry<T>::unpack(p.row.vec(i), x);
 #pragma unroll
-      for (int e = 0; e < N; ++e) key[e] = order_key(x[e], row.index(i) + e);
+      for (int e = 0; e < N; ++e) key[e] = order_key(x[e], p.row.index(i) + e);
     }
     uint64_t mine = key[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) mine = key[e] > mine ? key[e] : mine;
-    best[tid] = mine;
-    if (tid == 0) { *count = 0; best[kThreads] = 0; }
+    if (!__syncthreads_or(have < top || mine > l.kept[top - 1])) continue;
+    l.best[tid] = mine;
+    if (tid == 0) { l.count = 0; l.best[kThreads] = 0; }
     __syncthreads();
     int rank = 0;
-    for (int j = 0; j < kThreads; ++j) rank += best[j] > mine;
-    if (rank == top - 1 && mine) best[kThreads] = mine;      // keys differ, but for the zeros of idle threads
+    for (int j = 0; j < kThreads; ++j) rank += l.best[j] > mine;
+    if (rank == top - 1 && mine) l.best[kThreads] = mine;      // keys differ, but for the zeros of idle threads
     __syncthreads();
-    uint64_t bound = best[kThreads];
-    if (have == top && kept[top - 1] > bound) bound = kept[top - 1] + 1;
+    uint64_t bound = l.best[kThreads];
+    if (have == top && l.kept[top - 1] > bound) bound = l.kept[top - 1] + 1;
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (key[e] && key[e] >= bound) found[atomicAdd(count, 1)] = key[e];
+      if (key[e] && key[e] >= bound) l.found[atomicAdd(&l.count, 1)] = key[e];     // at most top * N
+    if (tid < have) l.found[kFound - 1 - tid] = l.kept[tid];
     __syncthreads();
-    const int n = *count;                        // at most top threads times N
-    if (n) {
-      uint64_t keep[3] = {0, 0, 0};
-      int at[3];
-#pragma unroll
-      for (int u = 0; u < 3; ++u) {
-        const int q = u * kThreads + tid;
-        if (q < n + have) {
-          const uint64_t v = q < n ? found[q] : kept[q - n];
-          int r = 0;
-          for (int j = 0; j < n; ++j) r += found[j] > v;
-          for (int j = 0; j < have; ++j) r += kept[j] > v;
-          keep[u] = v; at[u] = r;
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < 3; ++u)
-        if (keep[u] && at[u] < top) kept[at[u]] = keep[u];
-      have = have + n < top ? have + n : top;
-    }
+    const int n = l.count;
+    if (tid < have) l.found[n + tid] = l.found[kFound - 1 - tid];
+    __syncthreads();
+    rank_found(l, n + have, top);
+    have = have + n < top ? have + n : top;
     __syncthreads();
   }
-  if (tid >= have && tid < top) kept[tid] = 0;
+  if (tid >= have && tid < top) l.kept[tid] = 0;
   __syncthreads();
 }
 
-// The sums relative to the row's largest logit, which is what is put out: 1 <= s, and the entropy log s - t / s
-// has no terms larger than need be.  `far` rows are at the end of the type's range, where c z overflows: differences first.
+// What of `found` reaches the bound of the threads' largest entries, ranked.  Every thread has written its `most`.
+// False where more was found than could be listed.
+__device__ __forceinline__ bool select_found(Select& l, int top) {
+  __syncthreads();
+  const int n = l.count;
+  if (n > kFound) return false;
+  const uint64_t bound = (uint64_t)wave_bound(l.most, top) << 48;
+  // compacted in place: a thread's keys are in registers before the first is written
+  uint64_t key[kFound / kThreads];
+#pragma unroll
+  for (int u = 0; u < kFound / kThreads; ++u) {
+    const int q = u * kThreads + threadIdx.x;
+    key[u] = q < n ? l.found[q] : 0;
+  }
+  if (threadIdx.x == 0) l.chosen = 0;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kFound / kThreads; ++u)
+    if (key[u] && key[u] >= bound) l.found[atomicAdd(&l.chosen, 1)] = key[u];
+  __syncthreads();
+  rank_found(l, l.chosen, top);
+  __syncthreads();
+  return true;
+}
+
+template <int N>
+__device__ __forceinline__ void list_entries(Select& l, const float (&x)[N], int first, float bound) {
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (x[e] >= bound) {
+      const int q = atomicAdd(&l.count, 1);
+      if (q < kFound) l.found[q] = order_key(x[e], first + e);
+    }
+}
+
+// The sums relative to the piece's largest logit: 1 <= s, and the entropy log s - t / s has no terms larger than need be.
+// Pieces at the end of the type's range, where c z overflows, are read again, differences first.
 template <typename T>
-__device__ Sums row_sums(const RowSpan<T>& row, const Sums& mine, float c, float (*part)[4]) {
+__device__ __forceinline__ Sums piece_sums(const Piece<T>& p, const Sums& mine, float c, float (*part)[4]) {
   Sums a = block_sums(mine, part);
   const bool far = fabsf(a.m * c) > 1.0e30f && fabsf(a.m) < INFINITY;
+  if (a.m == -INFINITY) return a;                    // nothing but masked entries (s = 0) and NaN
   if (!far) {
     const float by = -fmaf(a.m, c, -a.r), f = fast_exp2(by);
     a.t = f * fmaf(a.s, by, a.t);
@@ -165,10 +253,17 @@ __device__ Sums row_sums(const RowSpan<T>& row, const Sums& mine, float c, float
   }
   __syncthreads();
   Sums b = {0.f, 0.f, 0.f, a.m};
-  for (int i = threadIdx.x; i < row.n; i += kThreads) {
-    const float d = (Entry<T>::one(row.p + i) - a.m) * c, e = fast_exp2(d);
+  auto add = [&](float z) {
+    const float d = (z - a.m) * c, e = fast_exp2(d);
     b.s += e;
     b.t = fmaf(e, fmaxf(d, kNegBig), b.t);
+  };
+  if ((int)threadIdx.x < p.edge) add(Entry<T>::one(p.row.p + p.row.edge_index(threadIdx.x)));
+  for (int i = p.v0 + threadIdx.x; i < p.v1; i += kThreads) {
+    float x[Entry<T>::kPerVec];
+    Entry<T>::unpack(p.row.vec(i), x);
+#pragma unroll
+    for (int e = 0; e < Entry<T>::kPerVec; ++e) add(x[e]);
   }
   return block_sums(b, part);
 }
@@ -207,32 +302,164 @@ __device__ void finish_row(const LogpArgs& a, int64_t row, const Sums& sum, cons
   }
 }
 
+// One pass over the row, kStep vectors to a thread at a time.  What bounds it is the read of the logits.
+// The alternatives ride on the softmax's own maxima: the `top`-th largest of the threads' largest entries is a lower bound of the
+// `top`-th largest entry.  The first kStep vectors give one, what reaches it is listed (top V / (256 kStep 8) entries of rows in no
+// particular order), and at the end the threads' largest of all leave little more than `top` of these to rank.
+constexpr int kStep = 4;
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void token_logp_kernel(LogpArgs a) {
+__global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
   constexpr int N = Entry<T>::kPerVec;
-  __shared__ uint64_t kept[ADWIN_MAX_TOP], found[ADWIN_MAX_TOP * 8], best[kThreads + 1];
+  __shared__ Select l;
   __shared__ float part[kWaves][4];
-  __shared__ int count;
-  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x;
+  const int64_t r = blockIdx.x / (uint32_t)a.pieces;
+  const int piece = (int)(blockIdx.x - (uint32_t)r * (uint32_t)a.pieces);
   int bad;
   const int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
   Sums sum = no_sums();
   if (live) {
-    const RowSpan<T> row((const T*)a.z + r * a.ld, a.V);
-    if ((int)threadIdx.x < row.edge) {
-      const float x[1] = {Entry<T>::one(row.p + row.edge_index(threadIdx.x))};
-      add_entries(sum, x, a.c);
+    const Piece<T> p((const T*)a.z + r * a.ld, a.V, piece, a.pieces);
+    float bound = INFINITY;
+    if (tid == 0) l.count = 0;
+    float edge[1] = {-INFINITY};
+    if (tid < p.edge) {
+      edge[0] = Entry<T>::one(p.row.p + p.row.edge_index(tid));
+      add_entries(sum, edge, a.c);
     }
-    for (int i = threadIdx.x; i < row.vecs; i += kThreads) {
-      float x[N];
-      Entry<T>::unpack(row.vec(i), x);
-      add_entries(sum, x, a.c);
+    for (int i0 = p.v0; i0 < p.v1 || i0 == p.v0; i0 += kStep * kThreads) {
+      uint4 v[kStep];
+      const int n = p.v1 - i0 - tid;                // vectors at i0 + tid + 256 u for 256 u < n
+#pragma unroll
+      for (int u = 0; u < kStep; ++u)
+        if (kThreads * u < n) v[u] = p.row.vec(i0 + tid + kThreads * u);
+      float most[kStep];
+#pragma unroll
+      for (int u = 0; u < kStep; ++u) {
+        most[u] = -INFINITY;
+        if (kThreads * u < n) {
+          float x[N];
+          Entry<T>::unpack(v[u], x);
+          const float before = sum.m;
+          sum.m = -INFINITY;
+          add_entries(sum, x, a.c);
+          most[u] = sum.m;
+          sum.m = fmaxf(sum.m, before);
+        }
+      }
+      if (a.top > 0) {
+        if (i0 == p.v0) {
+          l.most[tid] = order_bits(sum.m) >> 16;    // a thread without entries: -inf
+          __syncthreads();
+          bound = bound_value(wave_bound(l.most, a.top));
+          if (tid < p.edge) list_entries(l, edge, p.row.edge_index(tid), bound);
+        }
+#pragma unroll
+        for (int u = 0; u < kStep; ++u)
+          if (kThreads * u < n && most[u] >= bound) {
+            float x[N];
+            Entry<T>::unpack(v[u], x);
+            list_entries(l, x, p.row.index(i0 + tid + kThreads * u), bound);
+          }
+      }
     }
-    sum = row_sums<T>(row, sum, a.c, part);
-    if (a.top > 0) select_top<T>(row, a.top, kept, found, best, &count);
+    if (a.top > 0) {
+      __syncthreads();                              // all have read the first bound
+      l.most[tid] = order_bits(sum.m) >> 16;
+      if (!select_found(l, a.top)) select_slowly(p, a.top, l);
+    }
+    sum = piece_sums(p, sum, a.c, part);
   }
-  finish_row<T>(a, r, sum, kept, live, bad);
+  if (a.pieces == 1) {
+    finish_row<T>(a, r, sum, l.kept, live, bad);
+    return;
+  }
+  if (!live) return;                                // the join sees that by itself
+  if (tid == 0) {
+    float* q = a.part + 4 * (int64_t)blockIdx.x;
+    q[0] = sum.m; q[1] = sum.s; q[2] = sum.t; q[3] = 0.f;
+  }
+  if (tid < a.top) a.keys[(int64_t)blockIdx.x * a.top + tid] = l.kept[tid];
 }
+
+// The pieces of a row, joined in their order.
+constexpr int kMaxPieces = 64;
+template <typename T>
+__global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
+  __shared__ Select l;
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x;
+  int bad;
+  const int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
+  Sums sum = no_sums();
+  if (live) {
+    const float4* part = (const float4*)a.part + r * a.pieces;
+    if (a.top > 0) {
+      const int n = a.pieces * a.top;
+      const uint64_t* keys = a.keys + r * a.pieces * a.top;
+      constexpr int kMine = kMaxPieces * ADWIN_MAX_TOP / kThreads;
+      uint64_t key[kMine], most = 0;
+#pragma unroll
+      for (int u = 0; u < kMine; ++u) {
+        key[u] = u * kThreads + tid < n ? keys[u * kThreads + tid] : 0;
+        most = key[u] > most ? key[u] : most;
+      }
+      if (tid == 0) l.count = 0;
+      l.most[tid] = (uint32_t)(most >> 48);
+      __syncthreads();
+      const uint64_t bound = (uint64_t)wave_bound(l.most, a.top) << 48;
+#pragma unroll
+      for (int u = 0; u < kMine; ++u)
+        if (key[u] && key[u] >= bound) {
+          const int q = atomicAdd(&l.count, 1);
+          if (q < kFound) l.found[q] = key[u];
+        }
+      __syncthreads();
+      if (l.count <= kFound) {
+        rank_found(l, l.count, a.top);
+      } else {                                      // ties in all pieces: every key against all others
+        for (int q = tid; q < n; q += kThreads) {
+          const uint64_t v = keys[q];
+          int rank = 0;
+          for (int j = 0; j < n; ++j) rank += keys[j] > v;
+          if (v && rank < a.top) l.kept[rank] = v;
+        }
+      }
+    }
+    sum.m = -INFINITY;
+    for (int i = 0; i < a.pieces; ++i) sum.m = fmaxf(sum.m, part[i].x);
+    sum.s = sum.t = 0.f;
+    for (int i = 0; i < a.pieces; ++i) {
+      const float4 q = part[i];
+      const float by = (q.x - sum.m) * a.c, f = fast_exp2(by);
+      sum.t = fmaf(f, fmaf(q.y, fmaxf(by, kNegBig), q.z), sum.t);
+      sum.s = fmaf(f, q.y, sum.s);
+    }
+    __syncthreads();
+  }
+  finish_row<T>(a, r, sum, l.kept, live, bad);
+}
+
+// Pieces of a row.  One for calls of many rows; few rows are cut so that there are 1,024 workgroups (four to a compute
+// unit), each with a step of its threads or more.
+static int logp_pieces(int64_t T, int32_t V, int32_t dtype) {
+  const int64_t step = (int64_t)kStep * kThreads * (dtype == ADWIN_DT_BF16 ? 8 : 4) / 2;
+  int64_t n = (1024 + T - 1) / (T > 0 ? T : 1);
+  if (n > V / step) n = V / step;
+  return (int)(n < 1 ? 1 : n > kMaxPieces ? kMaxPieces : n);
+}
+
+struct LogpLayout {
+  int pieces;
+  size_t o_keys, bytes;
+  explicit LogpLayout(const adwin_opd_logp_problem* p) {
+    pieces = logp_pieces(p->T, p->V, p->z_dtype);
+    const size_t n = pieces > 1 ? (size_t)p->T * pieces : 0;
+    o_keys = align_up(n * 4 * sizeof(float), 256);
+    bytes = align_up(o_keys + n * p->top * sizeof(uint64_t), 256);
+  }
+};
 
 // ---------------------------------------------------------------------------------------
 // dz_j = -p_j (a + g_H (log p_j + H)) / temperature, a = sum_g g_g, and g_g / temperature more at the given tokens, whose
@@ -345,7 +572,7 @@ extern "C" int adwin_opd_token_logp_workspace_bytes(const adwin_opd_logp_problem
   if (!bytes) return ADWIN_E_NULL;
   const int st = check_logp(p);
   if (st != ADWIN_OK) return st;
-  *bytes = 0;
+  *bytes = LogpLayout(p).bytes;
   return ADWIN_OK;
 }
 
@@ -356,16 +583,25 @@ extern "C" int adwin_opd_token_logp(const adwin_opd_logp_problem* p, void* works
   if (p->T == 0) return ADWIN_OK;
   if (!p->z || (p->G > 0 && !p->ids)) return ADWIN_E_NULL;
   if ((uintptr_t)p->z & entry_mask(p->z_dtype)) return ADWIN_E_ALIGN;
+  const LogpLayout L(p);
+  if (L.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < L.bytes)) return ADWIN_E_WORKSPACE;
   LogpArgs a{};
   a.z = p->z; a.ld = p->ld_z; a.T = p->T; a.V = p->V; a.G = p->G; a.top = p->top;
   a.temperature = p->temperature; a.c = (float)(1.4426950408889634 / (double)p->temperature);
   a.ids = p->ids; a.logp = p->logp; a.entropy = p->entropy; a.norm = p->norm; a.top_ids = p->top_ids;
   a.top_logp = p->top_logp; a.row_status = p->row_status;
   if (!a.top_ids && !a.top_logp) a.top = 0;
+  a.pieces = L.pieces; a.part = (float*)workspace; a.keys = (uint64_t*)((unsigned char*)workspace + L.o_keys);
   hipStream_t stream = (hipStream_t)hip_stream;
-  if (p->z_dtype == ADWIN_DT_BF16) token_logp_kernel<uint16_t><<<(unsigned)p->T, kThreads, 0, stream>>>(a);
-  else token_logp_kernel<float><<<(unsigned)p->T, kThreads, 0, stream>>>(a);
+  const unsigned blocks = (unsigned)(p->T * L.pieces);
+  if (p->z_dtype == ADWIN_DT_BF16) token_logp_kernel<uint16_t><<<blocks, kThreads, 0, stream>>>(a);
+  else token_logp_kernel<float><<<blocks, kThreads, 0, stream>>>(a);
   ADWIN_HIP_TRY(hipGetLastError());
+  if (L.pieces > 1) {
+    if (p->z_dtype == ADWIN_DT_BF16) join_logp_kernel<uint16_t><<<(unsigned)p->T, kThreads, 0, stream>>>(a);
+    else join_logp_kernel<float><<<(unsigned)p->T, kThreads, 0, stream>>>(a);
+    ADWIN_HIP_TRY(hipGetLastError());
+  }
   return ADWIN_OK;
 }
 
