@@ -58,15 +58,25 @@ __device__ __forceinline__ void move_ref(Sums& a, float r) {
   a.s *= f;
   a.r = r;
 }
+// fmaxf without the two instructions that quiet its operands
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float m;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(x), "v"(y), "v"(z));
+  return m;
+}
+// returns the largest of x
 template <int N>
-__device__ __forceinline__ void add_entries(Sums& a, const float (&x)[N], float c) {
+__device__ __forceinline__ float add_entries(Sums& a, const float (&x)[N], float c) {
   float m = x[0];
+  if constexpr (N > 1) m = max3(x[0], x[1], x[2]);
 #pragma unroll
-  for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
-  a.m = fmaxf(a.m, m);
+  for (int i = 3; i + 1 < N; i += 2) m = max3(m, x[i], x[i + 1]);
+  if constexpr (N > 1) m = max3(m, x[N - 1], x[N - 1]);
+  a.m = max3(a.m, m, m);
   if (m * c > a.r + kSlack) move_ref(a, ref_of(m, c));
 #pragma unroll
   for (int i = 0; i < N; ++i) add_one(a, x[i], c);
+  return m;
 }
 __device__ __forceinline__ void merge_sums(Sums& a, Sums b) {
   if (b.r > a.r) { const Sums x = a; a = b; b = x; }
@@ -117,7 +127,7 @@ struct Select {                    // in the LDS
 
 // A lower bound of the `top`-th largest of the 256 numbers in `most`, exact in 16 bits, by every wave: the bits from the
 // highest on, a bit stays where at least `top` numbers reach it.  0 where fewer than `top` are above 0.
-__device__ __forceinline__ uint32_t wave_bound(const uint32_t* most, int top) {
+__device__ __forceinline__ uint32_t wave_bound(const volatile uint32_t* most, int top) {
   const int lane = threadIdx.x & 63;
   uint32_t v[kWaves];
 #pragma unroll
@@ -228,14 +238,29 @@ __device__ __forceinline__ bool select_found(Select& l, int top) {
   return true;
 }
 
-template <int N>
-__device__ __forceinline__ void list_entries(Select& l, const float (&x)[N], int first, float bound) {
+__device__ __forceinline__ void list_key(Select& l, uint64_t key) {
+  const int q = atomicAdd(&l.count, 1);
+  if (q < kFound) l.found[q] = key;
+}
+// Entries of vector v that reach the bound; `first`: the index of the vector's first one.
+template <typename T>
+__device__ __forceinline__ void list_entries(Select& l, const uint4& v, int first, float bound) {
+  float x[Entry<T>::kPerVec];
+  Entry<T>::unpack(v, x);
+  uint32_t which = 0;
 #pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (x[e] >= bound) {
-      const int q = atomicAdd(&l.count, 1);
-      if (q < kFound) l.found[q] = order_key(x[e], first + e);
-    }
+  for (int e = 0; e < Entry<T>::kPerVec; ++e) which |= x[e] >= bound ? 1u << e : 0u;
+  uint32_t w0 = v.x, w1 = v.y, w2 = v.z, w3 = v.w;
+  asm("" : "+v"(w0), "+v"(w1), "+v"(w2), "+v"(w3));      // four registers, not an array that is indexed in memory
+  while (which) {
+    const int e = __ffs(which) - 1;
+    which &= which - 1;
+    const int at = e * (int)sizeof(T) / 4;
+    const uint32_t even = at & 2 ? w2 : w0, odd = at & 2 ? w3 : w1;
+    uint32_t w = at & 1 ? odd : even;
+    if constexpr (sizeof(T) == 2) w = e & 1 ? w & 0xffff0000u : w << 16;
+    list_key(l, order_key(__uint_as_float(w), first + e));
+  }
 }
 
 // The sums relative to the piece's largest logit: 1 <= s, and the entropy log s - t / s has no terms larger than need be.
@@ -268,26 +293,35 @@ __device__ __forceinline__ Sums piece_sums(const Piece<T>& p, const Sums& mine, 
   return block_sums(b, part);
 }
 
-// 1 where some id of the row is scored (or G = 0); every thread of the workgroup gets the answer
-__device__ __forceinline__ int row_is_scored(const int32_t* ids, int G, int V, int64_t row, int* bad) {
-  int id = -1;
-  if ((int)threadIdx.x < G) id = ids[row * G + threadIdx.x];
-  *bad = __syncthreads_or(id >= V);
-  return G == 0 ? 1 : __syncthreads_or(id >= 0 && id < V);
+// Whether some id of the row is scored (or G = 0), and whether one is beyond V: every wave looks for itself.
+struct RowIds { bool live, bad; };
+__device__ __forceinline__ RowIds row_ids(const int32_t* ids, int G, int V, int64_t row) {
+  RowIds is{G == 0, false};
+  for (int g0 = 0; g0 < G; g0 += 64) {
+    const int g = g0 + (threadIdx.x & 63);
+    const int id = g < G ? ids[row * G + g] : -1;
+    is.live = is.live || __ballot(id >= 0 && id < V) != 0;
+    is.bad = is.bad || __ballot(id >= V) != 0;
+  }
+  return is;
 }
 
+// The logit of thread g's given token, g < G; masked where it is not scored.
 template <typename T>
-__device__ void finish_row(const LogpArgs& a, int64_t row, const Sums& sum, const uint64_t* kept, int live, int bad) {
-  const T* z = (const T*)a.z + row * a.ld;
+__device__ __forceinline__ float given_logit(const LogpArgs& a, int64_t row, bool* scored) {
+  const int id = (int)threadIdx.x < a.G ? a.ids[row * a.G + threadIdx.x] : -1;
+  *scored = id >= 0 && id < a.V;
+  return *scored ? Entry<T>::one((const T*)a.z + row * a.ld + id) : -INFINITY;
+}
+
+__device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const Sums& sum, const uint64_t* kept, RowIds is,
+                                           float given, bool scored) {
   const int tid = threadIdx.x;
   const float s = sum.s;
-  const bool fine = live && s > 0.f && s < INFINITY && fabsf(sum.m) < INFINITY;
+  const bool fine = is.live && s > 0.f && s < INFINITY && fabsf(sum.m) < INFINITY;
   const float ls = fine ? logf(s) : 0.f;
   if (tid < a.G && a.logp) {
-    const int id = a.ids[row * a.G + tid];
-    float v = 0.f;
-    if (fine && id >= 0 && id < a.V) v = (Entry<T>::one(z + id) - sum.m) / a.temperature - ls;
-    a.logp[row * a.G + tid] = v;
+    a.logp[row * a.G + tid] = fine && scored ? (given - sum.m) / a.temperature - ls : 0.f;
   }
   if (tid < a.top) {
     const uint64_t k = kept[tid];
@@ -298,28 +332,30 @@ __device__ void finish_row(const LogpArgs& a, int64_t row, const Sums& sum, cons
   if (tid == 0) {
     if (a.entropy) a.entropy[row] = fine ? fmaxf(0.f, fmaf(-kLn2, sum.t / s, ls)) : 0.f;
     if (a.norm) { a.norm[2 * row] = fine ? sum.m : 0.f; a.norm[2 * row + 1] = fine ? s : 0.f; }
-    if (a.row_status) a.row_status[row] = (bad ? ADWIN_DEV_BAD_ID : 0) | (live && !fine ? ADWIN_DEV_NONFINITE : 0);
+    if (a.row_status) a.row_status[row] = (is.bad ? ADWIN_DEV_BAD_ID : 0) | (is.live && !fine ? ADWIN_DEV_NONFINITE : 0);
   }
 }
 
 // One pass over the row, kStep vectors to a thread at a time.  What bounds it is the read of the logits.
 // The alternatives ride on the softmax's own maxima: the `top`-th largest of the threads' largest entries is a lower bound of the
-// `top`-th largest entry.  The first kStep vectors give one, what reaches it is listed (top V / (256 kStep 8) entries of rows in no
-// particular order), and at the end the threads' largest of all leave little more than `top` of these to rank.
+// `top`-th largest entry.  The first kStep vectors give one, what reaches it is listed (the bound is taken anew when twice as much
+// has been read), and at the end the threads' largest of all leave little more than `top` of these to rank.
 constexpr int kStep = 4;
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
   constexpr int N = Entry<T>::kPerVec;
   __shared__ Select l;
+  __shared__ float shared_bound;
   __shared__ float part[kWaves][4];
   const int tid = threadIdx.x;
   const int64_t r = blockIdx.x / (uint32_t)a.pieces;
   const int piece = (int)(blockIdx.x - (uint32_t)r * (uint32_t)a.pieces);
-  int bad;
-  const int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
+  const RowIds is = row_ids(a.ids, a.G, a.V, r);
   Sums sum = no_sums();
-  if (live) {
+  float given = 0.f;
+  bool scored = false;
+  if (is.live) {
     const Piece<T> p((const T*)a.z + r * a.ld, a.V, piece, a.pieces);
     float bound = INFINITY;
     if (tid == 0) l.count = 0;
@@ -328,40 +364,80 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       edge[0] = Entry<T>::one(p.row.p + p.row.edge_index(tid));
       add_entries(sum, edge, a.c);
     }
-    for (int i0 = p.v0; i0 < p.v1 || i0 == p.v0; i0 += kStep * kThreads) {
-      uint4 v[kStep];
-      const int n = p.v1 - i0 - tid;                // vectors at i0 + tid + 256 u for 256 u < n
+    const int last = p.v1 - tid;                    // a thread's vectors: p.v0 + tid + 256 k below p.v1
+    // whole steps, whose loads stand in no branch: the wait for a vector then leaves the younger ones in flight
+    const int whole = (p.v1 - p.v0) / (kStep * kThreads);
+    int i0 = p.v0;
+    uint4 v[kStep];
+    auto load = [&](int u) { v[u] = p.row.template vec<PAST>(i0 + tid + kThreads * u); };
+    auto load_any = [&](int u) {
+      v[u] = Entry<T>::none();
+      if (i0 + kThreads * u < last) load(u);
+    };
+    auto add = [&](int u) {
+      float x[N];
+      Entry<T>::unpack(v[u], x);
+      return add_entries(sum, x, a.c);
+    };
+    if (whole > 0) {
+#pragma unroll
+      for (int u = 0; u < kStep; ++u) load(u);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kStep; ++u) load_any(u);
+    }
+    if (a.pieces == 1) given = given_logit<T>(a, r, &scored);
+    // the first vectors, which give the first bound and are then gone through again
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) add(u);
+    if (a.top > 0) {
+      l.most[tid] = order_bits(sum.m) >> 16;        // a thread without entries: -inf
+      __syncthreads();
+      bound = bound_value(wave_bound(l.most, a.top));
+      if (tid == 0) shared_bound = bound;
+      if (tid < p.edge && edge[0] >= bound) list_key(l, order_key(edge[0], p.row.edge_index(tid)));
 #pragma unroll
       for (int u = 0; u < kStep; ++u)
-        if (kThreads * u < n) v[u] = p.row.vec(i0 + tid + kThreads * u);
-      float most[kStep];
+        if (i0 + kThreads * u < last) list_entries<T>(l, v[u], p.row.index(i0 + tid + kThreads * u), bound);
+    }
+    i0 += kStep * kThreads;
+    if (whole > 1) {
 #pragma unroll
-      for (int u = 0; u < kStep; ++u) {
-        most[u] = -INFINITY;
-        if (kThreads * u < n) {
-          float x[N];
-          Entry<T>::unpack(v[u], x);
-          const float before = sum.m;
-          sum.m = -INFINITY;
-          add_entries(sum, x, a.c);
-          most[u] = sum.m;
-          sum.m = fmaxf(sum.m, before);
-        }
-      }
+      for (int u = 0; u < kStep; ++u) load(u);
+    }
+    for (int step = 1; step < whole; ++step) {
       if (a.top > 0) {
-        if (i0 == p.v0) {
-          l.most[tid] = order_bits(sum.m) >> 16;    // a thread without entries: -inf
-          __syncthreads();
-          bound = bound_value(wave_bound(l.most, a.top));
-          if (tid < p.edge) list_entries(l, edge, p.row.edge_index(tid), bound);
+        // A new bound at steps 1, 2, 4, 8, ..., by one wave in turn.  An older maximum of a thread gives a bound as well,
+        // and so does an older bound: nobody waits.
+        if ((step & (step - 1)) == 0) {
+          *(volatile uint32_t*)&l.most[tid] = order_bits(sum.m) >> 16;
+          if ((tid >> 6) == (__ffs(step) & (kWaves - 1))) {
+            const float b = bound_value(wave_bound(l.most, a.top));
+            if ((tid & 63) == 0) *(volatile float*)&shared_bound = b;
+          }
         }
+        bound = fmaxf(bound, *(volatile float*)&shared_bound);
+      }
+      const int first = p.row.index(i0 + tid);
+      i0 += kStep * kThreads;
+      if (step + 1 < whole) {
+#pragma unroll
+        for (int u = 0; u < kStep; ++u) {
+          if (add(u) >= bound) list_entries<T>(l, v[u], first + kThreads * N * u, bound);
+          load(u);
+        }
+      } else {
 #pragma unroll
         for (int u = 0; u < kStep; ++u)
-          if (kThreads * u < n && most[u] >= bound) {
-            float x[N];
-            Entry<T>::unpack(v[u], x);
-            list_entries(l, x, p.row.index(i0 + tid + kThreads * u), bound);
-          }
+          if (add(u) >= bound) list_entries<T>(l, v[u], first + kThreads * N * u, bound);
+      }
+    }
+    if (whole > 0) {
+#pragma unroll
+      for (int u = 0; u < kStep; ++u) load_any(u);
+#pragma unroll
+      for (int u = 0; u < kStep; ++u) {
+        if (add(u) >= bound && i0 + kThreads * u < last) list_entries<T>(l, v[u], p.row.index(i0 + tid + kThreads * u), bound);
       }
     }
     if (a.top > 0) {
@@ -372,10 +448,10 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
     sum = piece_sums(p, sum, a.c, part);
   }
   if (a.pieces == 1) {
-    finish_row<T>(a, r, sum, l.kept, live, bad);
+    finish_row(a, r, sum, l.kept, is, given, scored);
     return;
   }
-  if (!live) return;                                // the join sees that by itself
+  if (!is.live) return;                                // the join sees that by itself
   if (tid == 0) {
     float* q = a.part + 4 * (int64_t)blockIdx.x;
     q[0] = sum.m; q[1] = sum.s; q[2] = sum.t; q[3] = 0.f;
@@ -390,10 +466,12 @@ __global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
   __shared__ Select l;
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
-  int bad;
-  const int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
+  const RowIds is = row_ids(a.ids, a.G, a.V, r);
   Sums sum = no_sums();
-  if (live) {
+  float given = 0.f;
+  bool scored = false;
+  if (is.live) {
+    given = given_logit<T>(a, r, &scored);
     const float4* part = (const float4*)a.part + r * a.pieces;
     if (a.top > 0) {
       const int n = a.pieces * a.top;
@@ -438,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
     }
     __syncthreads();
   }
-  finish_row<T>(a, r, sum, l.kept, live, bad);
+  finish_row(a, r, sum, l.kept, is, given, scored);
 }
 
 // Pieces of a row.  One for calls of many rows; few rows are cut so that there are 1,024 workgroups (four to a compute
@@ -488,8 +566,7 @@ __global__ __launch_bounds__(kThreads) void token_logp_grad_kernel(LogpGradArgs 
   __shared__ int id_of[ADWIN_MAX_GIVEN];
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x;
-  int bad;
-  int live = row_is_scored(a.ids, a.G, a.V, r, &bad);
+  bool live = row_ids(a.ids, a.G, a.V, r).live;
   const float s = live ? a.norm[2 * r + 1] : 0.f;
   live = live && s > 0.f;
   TO* out = (TO*)a.dz + r * a.ld_dz;
@@ -540,6 +617,12 @@ __global__ __launch_bounds__(kThreads) void token_logp_grad_kernel(LogpGradArgs 
       Entry<TO>::put(out + id, (sum + g.plain(at_id[tid])) * g.per_temperature);
     }
   }
+}
+
+// Whether an array of T x V is read (or written) past the caches: it is beyond the last-level cache of 256 MiB, so it has left
+// before anybody can find it there.
+static bool past_caches(int64_t T, int32_t V, int32_t dtype) {
+  return T * V * (dtype == ADWIN_DT_BF16 ? 2 : 4) > ((int64_t)320 << 20);
 }
 
 static bool known_temperature(float t) { return t >= 1.17549435e-38f && t <= 3.0e38f; }
@@ -594,8 +677,14 @@ extern "C" int adwin_opd_token_logp(const adwin_opd_logp_problem* p, void* works
   a.pieces = L.pieces; a.part = (float*)workspace; a.keys = (uint64_t*)((unsigned char*)workspace + L.o_keys);
   hipStream_t stream = (hipStream_t)hip_stream;
   const unsigned blocks = (unsigned)(p->T * L.pieces);
-  if (p->z_dtype == ADWIN_DT_BF16) token_logp_kernel<uint16_t><<<blocks, kThreads, 0, stream>>>(a);
-  else token_logp_kernel<float><<<blocks, kThreads, 0, stream>>>(a);
+  const bool past = past_caches(p->T, p->V, p->z_dtype);
+  if (p->z_dtype == ADWIN_DT_BF16) {
+    if (past) token_logp_kernel<uint16_t, true><<<blocks, kThreads, 0, stream>>>(a);
+    else token_logp_kernel<uint16_t, false><<<blocks, kThreads, 0, stream>>>(a);
+  } else {
+    if (past) token_logp_kernel<float, true><<<blocks, kThreads, 0, stream>>>(a);
+    else token_logp_kernel<float, false><<<blocks, kThreads, 0, stream>>>(a);
+  }
   ADWIN_HIP_TRY(hipGetLastError());
   if (L.pieces > 1) {
     if (p->z_dtype == ADWIN_DT_BF16) join_logp_kernel<uint16_t><<<(unsigned)p->T, kThreads, 0, stream>>>(a);

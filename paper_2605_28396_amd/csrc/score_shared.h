@@ -5,10 +5,13 @@
 
 namespace adwin {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // 16 bytes of a row: 8 entries of bf16, 4 of fp32.
 template <typename T> struct Entry;
 template <> struct Entry<uint16_t> {               // bf16
   static constexpr int kPerVec = 8;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }   // -inf
   static __device__ __forceinline__ float one(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -22,6 +25,7 @@ template <> struct Entry<uint16_t> {               // bf16
 };
 template <> struct Entry<float> {
   static constexpr int kPerVec = 4;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
@@ -47,7 +51,15 @@ struct RowSpan {
     edge = n - vecs * kPer;
   }
   __device__ __forceinline__ int edge_index(int e) const { return e < head ? e : e + vecs * kPer; }
-  __device__ __forceinline__ uint4 vec(int i) const { return ((const uint4*)(p + head))[i]; }
+  // PAST: lines that nobody reads again
+  template <bool PAST = false>
+  __device__ __forceinline__ uint4 vec(int i) const {
+    const u32x4* q = (const u32x4*)(p + head) + i;
+    u32x4 v;
+    if constexpr (PAST) v = __builtin_nontemporal_load(q);
+    else v = *q;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
   __device__ __forceinline__ int index(int i) const { return head + i * kPer; }
 };
 
