@@ -545,7 +545,7 @@ struct LogpLayout {
 // ---------------------------------------------------------------------------------------
 struct LogpGradArgs {
   const void* z; int64_t ld_z; void* dz; int64_t ld_dz; int64_t T;
-  int32_t V, G;
+  int32_t V, G, pieces;
   float c, per_temperature;
   const int32_t* ids; const float* norm; const float* g_logp; const float* entropy; const float* g_entropy;
 };
@@ -559,57 +559,85 @@ struct GradRow {
   }
 };
 
-template <typename TI, typename TO>
+// A workgroup per piece of a row.  What bounds it is the read of z and the write of dz, PAST the caches where they exceed them.
+template <typename TI, typename TO, bool PAST>
 __global__ __launch_bounds__(kThreads) void token_logp_grad_kernel(LogpGradArgs a) {
   constexpr int N = Entry<TI>::kPerVec;
   __shared__ float at_id[ADWIN_MAX_GIVEN], g_of[ADWIN_MAX_GIVEN];
   __shared__ int id_of[ADWIN_MAX_GIVEN];
-  const int64_t r = blockIdx.x;
+  const int64_t r = blockIdx.x / (uint32_t)a.pieces;
+  const int piece = (int)(blockIdx.x - (uint32_t)r * (uint32_t)a.pieces);
   const int tid = threadIdx.x;
   bool live = row_ids(a.ids, a.G, a.V, r).live;
   const float s = live ? a.norm[2 * r + 1] : 0.f;
   live = live && s > 0.f;
   TO* out = (TO*)a.dz + r * a.ld_dz;
-  const RowSpan<TI> row((const TI*)a.z + r * a.ld_z, a.V);
-  GradRow g{};
-  if (live) {
-    if (tid < a.G) {
-      const int id = a.ids[r * a.G + tid];
-      const bool in = id >= 0 && id < a.V;
-      id_of[tid] = in ? id : -1;
-      g_of[tid] = in ? a.g_logp[r * a.G + tid] : 0.f;
-      at_id[tid] = in ? Entry<TI>::one(row.p + id) : 0.f;
-    }
-    __syncthreads();
-    g.m = a.norm[2 * r]; g.c = a.c; g.per_s = 1.f / s; g.log_s = logf(s); g.per_temperature = a.per_temperature;
-    g.gh = a.g_entropy ? a.g_entropy[r] : 0.f;
-    g.H = a.g_entropy ? a.entropy[r] : 0.f;
-    for (int j = 0; j < a.G; ++j) g.a += g_of[j];
-  }
-  if (tid < row.edge) {
-    const int i = row.edge_index(tid);
-    Entry<TO>::put(out + i, live ? g.plain(Entry<TI>::one(row.p + i)) * g.per_temperature : 0.f);
-  }
-  const bool aligned = ((uintptr_t)(out + row.head) & 15) == 0;
-  for (int i = tid; i < row.vecs; i += kThreads) {
+  const Piece<TI> p((const TI*)a.z + r * a.ld_z, a.V, piece, a.pieces);
+  constexpr int kWhole = N * sizeof(TO) < 16 ? N * (int)sizeof(TO) : 16;
+  const bool whole = ((uintptr_t)(out + p.row.head) & (kWhole - 1)) == 0;
+  const int steps = (p.v1 - p.v0) / (kStep * kThreads);
+  if (!live) {
     float y[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = 0.f;
-    if (live) {
-      float x[N];
-      Entry<TI>::unpack(row.vec(i), x);
-#pragma unroll
-      for (int e = 0; e < N; ++e) y[e] = g.plain(x[e]) * g.per_temperature;
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) Entry<TO>::put(out + row.index(i) + e, y[e]);
+    if (tid < p.edge) Entry<TO>::put(out + p.row.edge_index(tid), 0.f);
+    for (int i = p.v0 + tid; i < p.v1; i += kThreads) put_entries<PAST>(out + p.row.index(i), y, whole);
+    return;
   }
-  (void)aligned;
-  if (!live) return;
-  __syncthreads();                               // the row's stores come before those of the given tokens
+  uint4 v[kStep];
+  int i0 = p.v0;
+  auto load = [&](int u) { v[u] = p.row.template vec<PAST>(i0 + tid + kThreads * u); };
+  if (steps > 0) {
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) load(u);
+  }
+  const float edge = tid < p.edge ? Entry<TI>::one(p.row.p + p.row.edge_index(tid)) : 0.f;
+  if (tid < a.G) {
+    const int id = a.ids[r * a.G + tid];
+    const bool in = id >= 0 && id < a.V;
+    id_of[tid] = in ? id : -1;
+    g_of[tid] = in ? a.g_logp[r * a.G + tid] : 0.f;
+    at_id[tid] = in ? Entry<TI>::one(p.row.p + id) : 0.f;
+  }
+  __syncthreads();
+  GradRow g{};
+  g.m = a.norm[2 * r]; g.c = a.c; g.per_s = 1.f / s; g.log_s = logf(s); g.per_temperature = a.per_temperature;
+  g.gh = a.g_entropy ? a.g_entropy[r] : 0.f;
+  g.H = a.g_entropy ? a.entropy[r] : 0.f;
+  for (int j = 0; j < a.G; ++j) g.a += g_of[j];
+  auto put = [&](int u, int first) {
+    float x[N];
+    Entry<TI>::unpack(v[u], x);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = g.plain(x[e]) * g.per_temperature;
+    put_entries<PAST>(out + first + kThreads * N * u, x, whole);
+  };
+  if (tid < p.edge) Entry<TO>::put(out + p.row.edge_index(tid), g.plain(edge) * g.per_temperature);
+  for (int step = 1; step < steps; ++step) {
+    const int first = p.row.index(i0 + tid);
+    i0 += kStep * kThreads;
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      put(u, first);
+      load(u);
+    }
+  }
+  if (steps > 0) {
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) put(u, p.row.index(i0 + tid));
+    i0 += kStep * kThreads;
+  }
+  for (; i0 < p.v1; i0 += kThreads)
+    if (i0 + tid < p.v1) {
+      load(0);
+      put(0, p.row.index(i0 + tid));
+    }
+  __syncthreads();                               // the piece's stores come before those of the given tokens
   if (tid < a.G && id_of[tid] >= 0) {
     const int id = id_of[tid];
-    bool first = true;
+    const bool in_edge = id < p.row.head || id >= p.row.index(p.row.vecs);
+    const bool mine = in_edge ? piece == 0 : id >= p.row.index(p.v0) && id < p.row.index(p.v1);
+    bool first = mine;
     for (int j = 0; j < tid; ++j) first = first && id_of[j] != id;
     if (first) {
       float sum = 0.f;
@@ -617,6 +645,14 @@ __global__ __launch_bounds__(kThreads) void token_logp_grad_kernel(LogpGradArgs 
       Entry<TO>::put(out + id, (sum + g.plain(at_id[tid])) * g.per_temperature);
     }
   }
+}
+
+// Pieces of a row, for 4,096 workgroups in a call, each with a step of its threads or more.
+static int grad_pieces(int64_t T, int32_t V, int32_t dtype) {
+  const int64_t step = (int64_t)kStep * kThreads * (dtype == ADWIN_DT_BF16 ? 8 : 4);
+  int64_t n = (4096 + T - 1) / T;
+  if (n > V / step) n = V / step;
+  return (int)(n < 1 ? 1 : n);
 }
 
 // Whether an array of T x V is read (or written) past the caches: it is beyond the last-level cache of 256 MiB, so it has left
@@ -706,12 +742,19 @@ extern "C" int adwin_opd_token_logp_grad(const adwin_opd_logp_grad_problem* p, v
   a.c = (float)(1.4426950408889634 / (double)p->temperature); a.per_temperature = 1.f / p->temperature;
   a.ids = p->ids; a.norm = p->norm; a.g_logp = p->g_logp; a.entropy = p->entropy; a.g_entropy = p->g_entropy;
   hipStream_t stream = (hipStream_t)hip_stream;
+  a.pieces = grad_pieces(p->T, p->V, p->z_dtype);
   const bool in16 = p->z_dtype == ADWIN_DT_BF16, out16 = p->dz_dtype == ADWIN_DT_BF16;
-  const unsigned blocks = (unsigned)p->T;
-  if (in16 && out16) token_logp_grad_kernel<uint16_t, uint16_t><<<blocks, kThreads, 0, stream>>>(a);
-  else if (in16) token_logp_grad_kernel<uint16_t, float><<<blocks, kThreads, 0, stream>>>(a);
-  else if (out16) token_logp_grad_kernel<float, uint16_t><<<blocks, kThreads, 0, stream>>>(a);
-  else token_logp_grad_kernel<float, float><<<blocks, kThreads, 0, stream>>>(a);
+  const bool past = past_caches(p->T, p->V, p->z_dtype) || past_caches(p->T, p->V, p->dz_dtype);
+  const unsigned blocks = (unsigned)(p->T * a.pieces);
+#define ADWIN_LAUNCH(...) token_logp_grad_kernel<__VA_ARGS__><<<blocks, kThreads, 0, stream>>>(a)
+#define ADWIN_LAUNCH_TYPES(PAST)                              \
+  if (in16 && out16) ADWIN_LAUNCH(uint16_t, uint16_t, PAST);  \
+  else if (in16) ADWIN_LAUNCH(uint16_t, float, PAST);         \
+  else if (out16) ADWIN_LAUNCH(float, uint16_t, PAST);        \
+  else ADWIN_LAUNCH(float, float, PAST);
+  if (past) { ADWIN_LAUNCH_TYPES(true) } else { ADWIN_LAUNCH_TYPES(false) }
+#undef ADWIN_LAUNCH_TYPES
+#undef ADWIN_LAUNCH
   ADWIN_HIP_TRY(hipGetLastError());
   return ADWIN_OK;
 }

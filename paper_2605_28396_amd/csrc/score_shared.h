@@ -18,9 +18,6 @@ template <> struct Entry<uint16_t> {               // bf16
 #pragma unroll
     for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
   }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-  }
   static __device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)pack_bf16(x, 0.f); }
 };
 template <> struct Entry<float> {
@@ -30,11 +27,38 @@ template <> struct Entry<float> {
   static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
-  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  }
   static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 };
+
+// y[0, N) to p: whole when p is a multiple of the bytes that they take (at most 16).
+template <bool PAST, int N>
+__device__ __forceinline__ void put_entries(float* p, const float (&y)[N], bool whole) {
+  if (whole) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      u32x4 v = {__float_as_uint(y[i]), __float_as_uint(y[i + 1]), __float_as_uint(y[i + 2]), __float_as_uint(y[i + 3])};
+      if constexpr (PAST) __builtin_nontemporal_store(v, (u32x4*)(p + i));
+      else *(u32x4*)(p + i) = v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = y[i];
+  }
+}
+template <bool PAST, int N>
+__device__ __forceinline__ void put_entries(uint16_t* p, const float (&y)[N], bool whole) {
+  typedef uint32_t Words __attribute__((ext_vector_type(N / 2)));
+  Words v;
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) v[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
+  if (whole) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, (Words*)p);
+    else *(Words*)p = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+  }
+}
 
 // A row of n entries at any address that suits its entries: `head` entries up to the first multiple of 16 bytes,
 // `vecs` whole vectors behind them, and `edge` entries outside the vectors (the head's and those after the last vector).
