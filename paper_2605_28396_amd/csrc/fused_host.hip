@@ -396,8 +396,10 @@ extern "C" int adwin_opd_init(void) {
   ADWIN_HIP_TRY(grad_kernels_opt_in());
   ADWIN_HIP_TRY(logits_kernels_opt_in());
   ADWIN_HIP_TRY(logits_static_setup());
+  ADWIN_HIP_TRY(quant_kernels_opt_in());
   (void)first_use_on_device(0);      // the calls need not repeat it on this device
   (void)first_use_on_device(1);
+  (void)first_use_on_device(2);
   return ADWIN_OK;
 }
 

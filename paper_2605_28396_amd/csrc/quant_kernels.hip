@@ -1,4 +1,5 @@
 // Rows to 8-bit integers, and the product of two arrays of such rows.
+#include "fused_shared.h"
 #include "score_shared.h"
 
 namespace adwin {
@@ -67,31 +68,274 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs p) {
 struct ProductArgs {
   const int8_t* h; const float* h_scale; const int8_t* W; const float* W_scale;
   void* z; int64_t ld_z; int64_t T;
-  int32_t V, pitch, token_tiles;
+  int32_t V, pitch;
+  int32_t token_tiles, vocab_tiles, strips, group;
+  int32_t whole;                   // rows of z lie and begin at multiples of 16 bytes
 };
 
-// v_mfma_i32_32x32x32_i8: lane l supplies row l % 32 of either operand, 16 bytes of k at half l / 32 (the sum does not depend
-// on which bytes these are, as long as both operands agree); result e of lane l is row 8 (e / 4) + 4 (l / 32) + e % 4 of A and row l % 32 of B.
-// A = entries of the head, B = tokens.  One wave per 32 x 32 block, straight from memory.
-template <typename T>
-__global__ __launch_bounds__(256) void quant_product_kernel(ProductArgs p) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t0 = (int64_t)(blockIdx.x % p.token_tiles) * 32;
-  const int64_t v0 = ((int64_t)(blockIdx.x / p.token_tiles) * 4 + wave) * 32;
-  if (v0 >= p.V) return;
-  const int64_t t = t0 + (lane & 31), v = v0 + (lane & 31);
-  const i32x4* W = (const i32x4*)(p.W + (v < p.V ? v : p.V - 1) * p.pitch) + (lane >> 5);   // rows beyond the last repeat it
-  const i32x4* h = (const i32x4*)(p.h + (t < p.T ? t : p.T - 1) * p.pitch) + (lane >> 5);
-  i32x16 acc = {};
-  for (int k = 0; k < p.pitch / 32; ++k) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(W[2 * k], h[2 * k], acc, 0, 0, 0);
-  if (t >= p.T) return;
-  const float s = p.h_scale[t];
-  T* z = (T*)p.z + t * p.ld_z;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int64_t j = v0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-    if (j < p.V) Entry<T>::put(z + j, (float)acc[e] * (s * p.W_scale[j]));
+// ---------------------------------------------------------------------------------------
+// The product, many tokens.  v_mfma_i32_32x32x32_i8: lane l supplies row l % 32 of either operand, 16 bytes of k of half
+// l / 32 (the sum does not depend on which bytes these are, as long as both operands agree); result e of lane l is row
+// 8 (e / 4) + 4 (l / 32) + e % 4 of A and row l % 32 of B.  A = entries of the head, B = tokens.
+//
+// Tile of 256 entries x 256 tokens, 2 x 2 waves of 128 x 128 (256 accumulators), k-steps of 128 bytes a row, staged by direct
+// global->LDS loads: a ring of three 32 KiB blocks for W, whose lines come from memory, and one of two for the tokens,
+// which the L2 holds.  Row r's 16-byte chunk c lies at chunk position c ^ (r / 2 % 8), so that the 16 lanes that read at a time
+// fall on different banks; tile row 8 q + 4 h + r of 32 holds entry 16 h + 4 q + r, which makes a lane's 16
+// results of a block 16 consecutive entries of z.
+// A workgroup keeps its tokens and walks a strip of vocabulary tiles; the k-steps of all of them form one pipeline: in step s
+// the blocks of step s + 2 are loaded, W behind the MFMAs of sub-steps 1 and 2 into the buffer that nobody reads any
+// more, the tokens behind those of sub-step 3 into the one that this step has finished.  The one barrier of a step stands before
+// its last sub-step, when every fragment of the step is in registers, and that sub-step's MFMAs cover the reads of the
+// next step's first fragments.  The order of the instructions is pinned, a read, a load or a piece of bookkeeping behind each MFMA.
+// ---------------------------------------------------------------------------------------
+constexpr int kQTile = 256;
+constexpr int kQBlock = kQTile * 128;                 // 32 KiB
+constexpr int kQRingB = 3 * kQBlock;                  // where the tokens' ring begins
+constexpr int kQLds = 5 * kQBlock;                    // 160 KiB
+
+typedef const __attribute__((address_space(3))) i32x4* LdsQFrag;
+__device__ __forceinline__ i32x4 q_frag(uint32_t addr, int row) { return *((LdsQFrag)(uintptr_t)addr + row * 8); }
+
+// Where the loads of the step after next come from: tile `tile` of the strip, k-step kt.
+struct QLoads {
+  const char* a; const char* b;                        // of that step
+  const char* a0; const char* b0;                      // of k-step 0 of its tile
+  int kt, tile;
+};
+
+// One k-step.  r_a, r_b: LDS address of the blocks that it reads plus the wave's KiB, on return those of the next step.
+template <bool FRESH>
+__device__ __forceinline__ void q_kstep(i32x16 (&acc)[4][4], i32x4 (&fa)[2][4], i32x4 (&fb)[2][4], uint32_t& r_a, uint32_t& r_b,
+                                        uint32_t a_begin, uint32_t b_begin, const uint32_t (&swA)[4], const uint32_t (&swB)[4],
+                                        const uint32_t (&voffa)[8], const uint32_t (&voffb)[8], QLoads& ld, int nk, int tiles,
+                                        int64_t tile_bytes, bool relaxed, int stores) {
+  const i32x16 zero = {};
+  uint32_t r_a_nx = 0, r_a_wr = 0, r_b_nx = 0, xa = 0, xb = 0;
+#define Q_FENCE __builtin_amdgcn_sched_barrier(0);
+#define Q_MM(KK, I, J)                                                                                           \
+  acc[I][J] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[(KK) & 1][I], fb[(KK) & 1][J],                            \
+                                                    FRESH && (KK) == 0 ? zero : acc[I][J], 0, 0, 0);             \
+  Q_FENCE
+  // behind MFMA M of sub-step KK
+#define Q_SIDE(KK, M)                                                                                            \
+  if constexpr ((M) < 8) {                                                                                       \
+    constexpr int nx = ((KK) + 1) & 3, f = (M) >> 1;                                                             \
+    if constexpr ((M) == 0) {                                                                                    \
+      xa = ((KK) < 3 ? r_a : r_a_nx) + swA[nx];                                                                  \
+      xb = ((KK) < 3 ? r_b : r_b_nx) + swB[nx];                                                                  \
+      asm volatile("" : "+v"(xa), "+v"(xb));                                                                     \
+    }                                                                                                            \
+    if constexpr (((M) & 1) == 0) fa[nx & 1][f] = q_frag(xa, 32 * f);                                            \
+    else fb[nx & 1][f] = q_frag(xb, 32 * f);                                                                     \
+    if constexpr ((KK) == 0 && (M) == 0) r_a_nx = ring_next<kQBlock>(r_a, a_begin, a_begin + 3 * kQBlock);       \
+    if constexpr ((KK) == 0 && (M) == 1) r_b_nx = ring_next<kQBlock>(r_b, b_begin, b_begin + 2 * kQBlock);       \
+    if constexpr ((KK) == 0 && (M) == 2) r_a_wr = ring_next<kQBlock>(r_a_nx, a_begin, a_begin + 3 * kQBlock);    \
+    Q_FENCE                                                                                                      \
+  } else if constexpr ((KK) == 0 && (M) == 8) {                                                                  \
+    const bool wrap = ld.kt + 1 == nk, on = wrap && ld.tile + 1 < tiles;                                         \
+    ld.kt = wrap ? 0 : ld.kt + 1;                                                                                \
+    ld.tile += on;                                                                                               \
+    ld.a0 += on ? tile_bytes : 0;                                                                                \
+    ld.a = wrap ? ld.a0 : ld.a + 128;                                                                            \
+    ld.b = wrap ? ld.b0 : ld.b + 128;                                                                            \
+    Q_FENCE                                                                                                      \
+  } else if constexpr (((KK) == 1 || (KK) == 2) && (M) >= 12) {                                                  \
+    dma16_at<(((KK) - 1) * 4 + (M) - 12) * 4096>(r_a_wr, voffa[(((KK) - 1) * 4 + (M) - 12) & 7], ld.a);          \
+    Q_FENCE                                                                                                      \
+  } else if constexpr ((KK) == 3 && (M) >= 8) {                                                                  \
+    dma16_at<((M) - 8) * 4096>(r_b, voffb[((M) - 8) & 7], ld.b);                                                 \
+    Q_FENCE                                                                                                      \
   }
+#define Q_ROW(KK, I, M0)                                                                            \
+  Q_MM(KK, I, 0) Q_SIDE(KK, (M0) + 0) Q_MM(KK, I, 1) Q_SIDE(KK, (M0) + 1)                           \
+  Q_MM(KK, I, 2) Q_SIDE(KK, (M0) + 2) Q_MM(KK, I, 3) Q_SIDE(KK, (M0) + 3)
+#define Q_SUB(KK) Q_ROW(KK, 0, 0) Q_ROW(KK, 1, 4) Q_ROW(KK, 2, 8) Q_ROW(KK, 3, 12)
+  Q_FENCE
+  Q_SUB(0)
+  Q_SUB(1)
+  Q_SUB(2)
+  // The next step's blocks have landed, and every wave has this step's fragments.  Loads return in order: the eight youngest,
+  // this step's of W, stay in flight, and in the first step of a tile the stores of the tile before, which came
+  // behind the loads that are waited for.
+  if (FRESH && relaxed) {
+    if (stores > 32) asm volatile("s_waitcnt vmcnt(63) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(40) lgkmcnt(0)" ::: "memory");
+  } else {
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+  }
+  __syncthreads();
+  Q_FENCE
+  Q_SUB(3)
+  r_a = r_a_nx;
+  r_b = r_b_nx;
+#undef Q_SUB
+#undef Q_ROW
+#undef Q_SIDE
+#undef Q_MM
+#undef Q_FENCE
+}
+
+// An accumulator as a number.  The constraint keeps it in its accumulator register until here.
+__device__ __forceinline__ float acc_read(int a) {
+  int v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+  return (float)v;
+}
+
+// 16 consecutive entries of z
+__device__ __forceinline__ void put16(float* z, const float (&y)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    ((u32x4*)z)[i] = u32x4{__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]), __float_as_uint(y[4 * i + 2]), __float_as_uint(y[4 * i + 3])};
+}
+__device__ __forceinline__ void put16(uint16_t* z, const float (&y)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    ((u32x4*)z)[i] = u32x4{pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]),
+                           pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7])};
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  int strip, tt;
+  strip_and_tile(xcd_contiguous_id(blockIdx.x, gridDim.x), p.group, p.strips, p.token_tiles, &strip, &tt);
+  const int vt0 = (int)((int64_t)p.vocab_tiles * strip / p.strips), vt1 = (int)((int64_t)p.vocab_tiles * (strip + 1) / p.strips);
+  if (vt0 >= vt1) return;
+  const int64_t t0 = (int64_t)tt * kQTile;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const uint32_t a_begin = lds0 + wave * 1024u, b_begin = a_begin + kQRingB;
+  const int nk = p.pitch / 128;
+  const int64_t tile_bytes = (int64_t)kQTile * p.pitch;
+
+  // lane offsets of the wave's eight loads of a block: tile rows 32 d + 8 wave + lane / 8
+  const uint32_t chunk = (uint32_t)((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 16u;
+  const int e0 = 16 * half + 4 * wave + ((lane >> 3) & 3);
+  uint32_t voffa[8], voffb[8];
+  auto rows_of_w = [&](int tile) {                       // rows beyond V repeat the last one
+    const int left = p.V - tile * kQTile - 1;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      const int v = 32 * d + e0;
+      voffa[d] = (uint32_t)(v < left ? v : left) * (uint32_t)p.pitch + chunk;
+      asm volatile("" : "+v"(voffa[d]));
+    }
+  };
+  rows_of_w(vt0);
+#pragma unroll
+  for (int d = 0; d < 8; ++d) {
+    const int64_t t = 32 * d + 8 * wave + (lane >> 3), left = p.T - t0 - 1;
+    voffb[d] = (uint32_t)(t < left ? t : left) * (uint32_t)p.pitch + chunk;
+    asm volatile("" : "+v"(voffb[d]));
+  }
+  uint32_t swA[4], swB[4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) {
+    const uint32_t at = (lane & 31) * 128u + (uint32_t)(((2 * kk + half) ^ (lane >> 1)) & 7) * 16u - wave * 1024u;
+    swA[kk] = at + wa * (kQBlock / 2);
+    swB[kk] = at + wb * (kQBlock / 2);
+  }
+  // the lane's tokens: their scales, their rows of z from the lane's half on, how many there are
+  float sh[4];
+  T* z[4];
+  int columns = 0;
+#pragma unroll
+  for (int fn = 0; fn < 4; ++fn) {
+    const int64_t t = t0 + 128 * wb + 32 * fn + (lane & 31);
+    sh[fn] = p.h_scale[t < p.T ? t : p.T - 1];
+    z[fn] = (T*)p.z + t * p.ld_z + 16 * half;
+    columns += t < p.T;
+    asm volatile("" : "+v"(sh[fn]));                     // waited for here, not behind the loads that follow
+  }
+
+  QLoads ld;
+  ld.a0 = ld.a = (const char*)p.W + vt0 * tile_bytes;
+  ld.b0 = ld.b = (const char*)p.h + t0 * p.pitch;
+  ld.kt = 0; ld.tile = 0;
+  const int tiles = vt1 - vt0;
+  int partial = p.V - vt1 * kQTile < 0 ? tiles - 1 : -1;      // the strip's tile that V ends in
+  auto load_step = [&](uint32_t ra, uint32_t rb) {
+#define Q_LOAD(D) dma16_at<(D) * 4096>(ra, voffa[D], ld.a);
+    Q_LOAD(0) Q_LOAD(1) Q_LOAD(2) Q_LOAD(3) Q_LOAD(4) Q_LOAD(5) Q_LOAD(6) Q_LOAD(7)
+#undef Q_LOAD
+#define Q_LOAD(D) dma16_at<(D) * 4096>(rb, voffb[D], ld.b);
+    Q_LOAD(0) Q_LOAD(1) Q_LOAD(2) Q_LOAD(3) Q_LOAD(4) Q_LOAD(5) Q_LOAD(6) Q_LOAD(7)
+#undef Q_LOAD
+  };
+  // steps 0 and 1
+  load_step(a_begin, b_begin);
+  if (nk > 1) { ld.kt = 1; ld.a += 128; ld.b += 128; }
+  else if (tiles > 1) { ld.tile = 1; ld.a0 += tile_bytes; ld.a = ld.a0; if (partial == 1) rows_of_w(vt0 + 1); }
+  load_step(a_begin + kQBlock, b_begin + kQBlock);
+  asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+  __syncthreads();
+  i32x16 acc[4][4];
+  i32x4 fa[2][4], fb[2][4];
+  uint32_t r_a = a_begin, r_b = b_begin;
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    fa[0][f] = q_frag(r_a + swA[0], 32 * f);
+    fb[0][f] = q_frag(r_b + swB[0], 32 * f);
+  }
+  bool relaxed = false;
+  const int stores = sizeof(T) == 2 ? 32 : 64;
+  for (int i = 0; i < tiles; ++i) {
+    // the loads of a step go into the tile that V ends in
+    auto into_last = [&]() __attribute__((always_inline)) {
+      if (ld.kt + 1 == nk && ld.tile + 1 == partial) rows_of_w(vt0 + partial);
+    };
+    into_last();
+    q_kstep<true>(acc, fa, fb, r_a, r_b, a_begin, b_begin, swA, swB, voffa, voffb, ld, nk, tiles, tile_bytes, relaxed, stores);
+    for (int kt = 1; kt < nk; ++kt) {
+      into_last();
+      q_kstep<false>(acc, fa, fb, r_a, r_b, a_begin, b_begin, swA, swB, voffa, voffb, ld, nk, tiles, tile_bytes, false, 0);
+    }
+    const int64_t v0 = (int64_t)(vt0 + i) * kQTile + 128 * wa;
+    const int left = (int)(p.V - v0);                    // may be 0 or less
+#pragma unroll
+    for (int fm = 0; fm < 4; ++fm) {
+      if (32 * fm < left) {
+        float sv[16];
+        if (32 * fm + 32 <= left) {
+          // the scales of the wave's 32 entries through the scalar cache, which the vector loads in flight do not hold up
+          typedef const __attribute__((address_space(4))) float* Scales;
+          const Scales s = (Scales)(uintptr_t)(p.W_scale + v0 + 32 * fm);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sv[e] = half ? s[16 + e] : s[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = 32 * fm + 16 * half + e;
+            sv[e] = p.W_scale[v0 + (j < left ? j : left - 1)];
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int n = left - 32 * fm - 16 * half;        // of the lane's 16 entries
+#pragma unroll
+        for (int fn = 0; fn < 4; ++fn) {
+          float y[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] = acc_read(acc[fm][fn][e]) * (sh[fn] * sv[e]);
+          T* at = z[fn] + v0 + 32 * fm;
+          asm volatile("" : "+v"(at));
+          if (fn < columns) {
+            if (p.whole && n >= 16) put16(at, y);
+            else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (e < n) Entry<T>::put(at + e, y[e]);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    relaxed = p.whole && left >= 128 && t0 + kQTile <= p.T;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads that nobody reads may still be writing the LDS
 }
 
 static int check_quant(const adwin_opd_quant_problem* p) {
@@ -118,6 +362,28 @@ struct QuantLayout {
     bytes = align_up(o_scale + sizeof(float) * (size_t)T, 256);
   }
 };
+
+// Strips of the vocabulary for `tiles` token tiles: one workgroup occupies a compute unit, so that what counts is the number of
+// rounds times the tiles of the longest strip.
+static int product_strips(int64_t tiles, int32_t vocab_tiles) {
+  int64_t best = 0;
+  int strips = 1;
+  for (int s = 1; s <= vocab_tiles && s <= 256; ++s) {
+    const int64_t cost = (tiles * s + 255) / 256 * ((vocab_tiles + s - 1) / s);
+    if (best == 0 || cost < best) { best = cost; strips = s; }
+  }
+  return strips;
+}
+
+// large dynamic LDS of the product, once per device
+hipError_t quant_kernels_opt_in() {
+  for (const void* k : {(const void*)quant_tile_kernel<uint16_t>, (const void*)quant_tile_kernel<float>}) {
+    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kQLds);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+static hipError_t quant_opt_in() { return first_use_on_device(2) ? quant_kernels_opt_in() : hipSuccess; }
 
 static hipError_t launch_quant_rows(const QuantArgs& a, int32_t dtype, hipStream_t st) {
   const unsigned blocks = (unsigned)((a.N + 3) / 4);
@@ -164,12 +430,21 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
   float* scale = (float*)((unsigned char*)workspace + L.o_scale);
   const QuantArgs rows{p->h, p->ld_h, p->T, p->H, ADWIN_QUANT_PITCH(p->H), q, scale, p->row_status};
   ADWIN_HIP_TRY(launch_quant_rows(rows, p->h_dtype, stream));
-  ProductArgs a{q, scale, p->W_q, p->W_scale, p->z, p->ld_z, p->T, p->V, ADWIN_QUANT_PITCH(p->H), 0};
-  a.token_tiles = (int32_t)((p->T + 31) / 32);
-  const int64_t blocks = (int64_t)a.token_tiles * ((p->V + 127) / 128);
-  if (blocks >= kMaxRows) return ADWIN_E_SHAPE;
-  if (p->z_dtype == ADWIN_DT_BF16) quant_product_kernel<uint16_t><<<(unsigned)blocks, 256, 0, stream>>>(a);
-  else quant_product_kernel<float><<<(unsigned)blocks, 256, 0, stream>>>(a);
+  ProductArgs a{};
+  a.h = q; a.h_scale = scale; a.W = p->W_q; a.W_scale = p->W_scale; a.z = p->z; a.ld_z = p->ld_z; a.T = p->T; a.V = p->V;
+  a.pitch = ADWIN_QUANT_PITCH(p->H);
+  const int64_t size = p->z_dtype == ADWIN_DT_BF16 ? 2 : 4;
+  a.whole = ((uintptr_t)p->z & 15) == 0 && (p->ld_z * size & 15) == 0;
+  const int64_t tiles = (p->T + kQTile - 1) / kQTile;
+  a.token_tiles = (int32_t)tiles;
+  a.vocab_tiles = (p->V + kQTile - 1) / kQTile;
+  a.strips = product_strips(tiles, a.vocab_tiles);
+  a.group = 4;
+  if (tiles * a.strips >= kMaxRows) return ADWIN_E_SHAPE;
+  const unsigned blocks = (unsigned)(tiles * a.strips);
+  ADWIN_HIP_TRY(quant_opt_in());
+  if (p->z_dtype == ADWIN_DT_BF16) quant_tile_kernel<uint16_t><<<blocks, 256, kQLds, stream>>>(a);
+  else quant_tile_kernel<float><<<blocks, 256, kQLds, stream>>>(a);
   ADWIN_HIP_TRY(hipGetLastError());
   return ADWIN_OK;
 }
