@@ -304,13 +304,19 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
           typedef const __attribute__((address_space(4))) float* Scales;
           const Scales s = (Scales)(uintptr_t)(p.W_scale + v0 + 32 * fm);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sv[e] = half ? s[16 + e] : s[e];
+          for (int e = 0; e < 16; ++e) {
+            float lo = s[e], hi = s[16 + e];
+            asm("" : "+s"(lo), "+s"(hi));                // and not one load from an address that differs from lane to lane
+            sv[e] = half ? hi : lo;
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int j = 32 * fm + 16 * half + e;
             sv[e] = p.W_scale[v0 + (j < left ? j : left - 1)];
           }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(sv[e]));    // waited for here: whole blocks wait for no store
         }
         __builtin_amdgcn_sched_barrier(0);
         const int n = left - 32 * fm - 16 * half;        // of the lane's 16 entries
