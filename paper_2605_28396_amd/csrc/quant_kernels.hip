@@ -183,17 +183,19 @@ __device__ __forceinline__ float acc_read(int a) {
   return (float)v;
 }
 
-// 16 consecutive entries of z
-__device__ __forceinline__ void put16(float* z, const float (&y)[16]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    ((u32x4*)z)[i] = u32x4{__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]), __float_as_uint(y[4 * i + 2]), __float_as_uint(y[4 * i + 3])};
+// entry e of 16 bytes of a row of z
+template <typename T>
+__device__ __forceinline__ T entry_of(const u32x4& v, int e) {
+  if constexpr (sizeof(T) == 2) return (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+  else return __uint_as_float(v[e]);
 }
-__device__ __forceinline__ void put16(uint16_t* z, const float (&y)[16]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    ((u32x4*)z)[i] = u32x4{pack_bf16(y[8 * i], y[8 * i + 1]), pack_bf16(y[8 * i + 2], y[8 * i + 3]),
-                           pack_bf16(y[8 * i + 4], y[8 * i + 5]), pack_bf16(y[8 * i + 6], y[8 * i + 7])};
+
+// 16 bytes of a row of z
+__device__ __forceinline__ u32x4 pack16(const float* y, float) {
+  return u32x4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+}
+__device__ __forceinline__ u32x4 pack16(const float* y, uint16_t) {
+  return u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
 }
 
 template <typename T>
@@ -238,18 +240,15 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
     swA[kk] = at + wa * (kQBlock / 2);
     swB[kk] = at + wb * (kQBlock / 2);
   }
-  // the lane's tokens: their scales, their rows of z from the lane's half on, how many there are
-  float sh[4];
-  T* z[4];
-  int columns = 0;
+  float sh[4];                                           // scales of the lane's tokens
 #pragma unroll
   for (int fn = 0; fn < 4; ++fn) {
     const int64_t t = t0 + 128 * wb + 32 * fn + (lane & 31);
     sh[fn] = p.h_scale[t < p.T ? t : p.T - 1];
-    z[fn] = (T*)p.z + t * p.ld_z + 16 * half;
-    columns += t < p.T;
     asm volatile("" : "+v"(sh[fn]));                     // waited for here, not behind the loads that follow
   }
+  // where the lane stores: token lane / 16, the entries of its chunk
+  T* const z = (T*)p.z + (t0 + (lane >> 4)) * p.ld_z + (lane & 15) * (int)(16 / sizeof(T));
 
   QLoads ld;
   ld.a0 = ld.a = (const char*)p.W + vt0 * tile_bytes;
@@ -293,53 +292,87 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
       into_last();
       q_kstep<false>(acc, fa, fb, r_a, r_b, a_begin, b_begin, swA, swB, voffa, voffb, ld, nk, tiles, tile_bytes, false, 0);
     }
+    // z.  A lane has 16 entries of a token, which as they are would go out as 16-byte pieces of 64 different rows.  A wave
+    // lays 32 tokens x 256 bytes into the LDS first and stores whole lines: into the KiBs that its own loads will fill of the
+    // block that the last step has read (row r's chunk c at chunk position c ^ (r % 16): 16 lanes on different banks either way).
     const int64_t v0 = (int64_t)(vt0 + i) * kQTile + 128 * wa;
     const int left = (int)(p.V - v0);                    // may be 0 or less
+    relaxed = p.whole && left >= 128 && t0 + kQTile <= p.T;
+    if (left <= 0) continue;
+    float sv[4][16];
+    if (left >= 128) {
+      // the scales of the wave's entries through the scalar cache, which the vector loads in flight do not hold up
+      typedef const __attribute__((address_space(4))) float* Scales;
+      const Scales s = (Scales)(uintptr_t)(p.W_scale + v0);
 #pragma unroll
-    for (int fm = 0; fm < 4; ++fm) {
-      if (32 * fm < left) {
-        float sv[16];
-        if (32 * fm + 32 <= left) {
-          // the scales of the wave's 32 entries through the scalar cache, which the vector loads in flight do not hold up
-          typedef const __attribute__((address_space(4))) float* Scales;
-          const Scales s = (Scales)(uintptr_t)(p.W_scale + v0 + 32 * fm);
+      for (int fm = 0; fm < 4; ++fm) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float lo = s[e], hi = s[16 + e];
-            asm("" : "+s"(lo), "+s"(hi));                // and not one load from an address that differs from lane to lane
-            sv[e] = half ? hi : lo;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = 32 * fm + 16 * half + e;
-            sv[e] = p.W_scale[v0 + (j < left ? j : left - 1)];
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(sv[e]));    // waited for here: whole blocks wait for no store
+        for (int e = 0; e < 16; ++e) {
+          float lo = s[32 * fm + e], hi = s[32 * fm + 16 + e];
+          asm volatile("" : "+s"(lo), "+s"(hi));         // and not one load from an address that differs from lane to lane
+          sv[fm][e] = half ? hi : lo;
+          asm volatile("" : "+v"(sv[fm][e]));
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int n = left - 32 * fm - 16 * half;        // of the lane's 16 entries
+      }
+    } else {
 #pragma unroll
-        for (int fn = 0; fn < 4; ++fn) {
+      for (int fm = 0; fm < 4; ++fm)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = 32 * fm + 16 * half + e;
+          sv[fm][e] = p.W_scale[v0 + (j < left ? j : left - 1)];
+        }
+#pragma unroll
+      for (int fm = 0; fm < 4; ++fm)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(sv[fm][e]));    // waited for here: whole tiles wait for no store
+    }
+    typedef __attribute__((address_space(3))) u32x4* LdsVec;
+    const uint32_t free = r_a == a_begin ? a_begin + 2 * kQBlock : r_a - kQBlock;
+    const uint32_t mine = free + (uint32_t)((lane & 31) >> 2) * 4096u + (lane & 3) * 256u;      // the lane's token
+    constexpr int kFms = sizeof(T) == 2 ? 4 : 2, kPer = 16 / sizeof(T);      // blocks of 32 entries to a row in the LDS
+    const int c = lane & 15;                             // reading, a lane has chunk c of rows 4 i + lane / 16
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int fn = 0; fn < 4; ++fn)
+#pragma unroll
+      for (int f0 = 0; f0 < 4; f0 += kFms) {
+#pragma unroll
+        for (int f = 0; f < kFms; ++f) {
           float y[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) y[e] = acc_read(acc[fm][fn][e]) * (sh[fn] * sv[e]);
-          T* at = z[fn] + v0 + 32 * fm;
-          asm volatile("" : "+v"(at));
-          if (fn < columns) {
-            if (p.whole && n >= 16) put16(at, y);
-            else {
+          for (int e = 0; e < 16; ++e) y[e] = acc_read(acc[f0 + f][fn][e]) * (sh[fn] * sv[f0 + f][e]);
 #pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (e < n) Entry<T>::put(at + e, y[e]);
-            }
+          for (int k = 0; k < 16 / kPer; ++k) {
+            const int at = (f * 32 + 16 * half) / kPer + k;
+            *(LdsVec)(uintptr_t)(mine + (uint32_t)((at ^ (lane & 15)) * 16)) = pack16(y + k * kPer, T{});
           }
           __builtin_amdgcn_sched_barrier(0);
         }
+        u32x4 row[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int r = 4 * k + (lane >> 4);
+          row[k] = *(LdsVec)(uintptr_t)(free + k * 4096u + (uint32_t)(lane >> 4) * 256u + (uint32_t)((c ^ (r & 15)) * 16));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int n = left - 32 * f0 - c * kPer;         // of the lane's entries
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int64_t t = t0 + 128 * wb + 32 * fn + 4 * k;
+          T* at = z + (t - t0) * p.ld_z + v0 + 32 * f0;
+          if (t + (lane >> 4) < p.T) {
+            if (p.whole && n >= kPer) *(u32x4*)at = row[k];
+            else {
+#pragma unroll
+              for (int e = 0; e < kPer; ++e)
+                if (e < n) at[e] = entry_of<T>(row[k], e);
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-    }
-    relaxed = p.whole && left >= 128 && t0 + kQTile <= p.T;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads that nobody reads may still be writing the LDS
 }
