@@ -247,8 +247,10 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
     sh[fn] = p.h_scale[t < p.T ? t : p.T - 1];
     asm volatile("" : "+v"(sh[fn]));                     // waited for here, not behind the loads that follow
   }
-  // where the lane stores: token lane / 16, the entries of its chunk
-  T* const z = (T*)p.z + (t0 + (lane >> 4)) * p.ld_z + (lane & 15) * (int)(16 / sizeof(T));
+  // where the lane stores first: token lane / 16 of the wave's, the entries of its chunk; and the tokens from there on
+  T* const z = (T*)p.z + (t0 + 128 * wb + (lane >> 4)) * p.ld_z + (lane & 15) * (int)(16 / sizeof(T));
+  const int64_t row_step = 4 * p.ld_z, rows_here = p.T - t0 - 128 * wb - (lane >> 4);
+  const int rows_left = (int)(rows_here < 128 ? rows_here : 128);
 
   QLoads ld;
   ld.a0 = ld.a = (const char*)p.W + vt0 * tile_bytes;
@@ -303,12 +305,14 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
     if (left >= 128) {
       // the scales of the wave's entries through the scalar cache, which the vector loads in flight do not hold up
       typedef const __attribute__((address_space(4))) float* Scales;
-      const Scales s = (Scales)(uintptr_t)(p.W_scale + v0);
+      uint64_t at = (uint64_t)(uintptr_t)(p.W_scale + v0);
 #pragma unroll
       for (int fm = 0; fm < 4; ++fm) {
+        asm volatile("" : "+s"(at));                     // 32 at a time
+        const Scales s = (Scales)(uintptr_t)at + 32 * fm;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float lo = s[32 * fm + e], hi = s[32 * fm + 16 + e];
+          float lo = s[e], hi = s[16 + e];
           asm volatile("" : "+s"(lo), "+s"(hi));         // and not one load from an address that differs from lane to lane
           sv[fm][e] = half ? hi : lo;
           asm volatile("" : "+v"(sv[fm][e]));
@@ -332,7 +336,11 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
     const uint32_t free = r_a == a_begin ? a_begin + 2 * kQBlock : r_a - kQBlock;
     const uint32_t mine = free + (uint32_t)((lane & 31) >> 2) * 4096u + (lane & 3) * 256u;      // the lane's token
     constexpr int kFms = sizeof(T) == 2 ? 4 : 2, kPer = 16 / sizeof(T);      // blocks of 32 entries to a row in the LDS
-    const int c = lane & 15;                             // reading, a lane has chunk c of rows 4 i + lane / 16
+    const int c = lane & 15;                             // reading, a lane has chunk c of rows 4 k + lane / 16
+    // formed anew for every tile: as invariants of the loop the 32 rows' addresses and masks do not fit the registers
+    T* at = z + v0;
+    int rows = rows_left;
+    asm volatile("" : "+v"(at), "+v"(rows));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int fn = 0; fn < 4; ++fn)
@@ -360,16 +368,17 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
         const int n = left - 32 * f0 - c * kPer;         // of the lane's entries
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int64_t t = t0 + 128 * wb + 32 * fn + 4 * k;
-          T* at = z + (t - t0) * p.ld_z + v0 + 32 * f0;
-          if (t + (lane >> 4) < p.T) {
-            if (p.whole && n >= kPer) *(u32x4*)at = row[k];
+          if (rows > 32 * fn + 4 * k) {
+            if (p.whole && n >= kPer) *(u32x4*)(at + 32 * f0) = row[k];
             else {
 #pragma unroll
               for (int e = 0; e < kPer; ++e)
-                if (e < n) at[e] = entry_of<T>(row[k], e);
+                if (e < n) at[32 * f0 + e] = entry_of<T>(row[k], e);
             }
           }
+          if (f0 + kFms == 4) at += row_step;
+          else if (k < 7) at += row_step;
+          else at -= 7 * row_step;
         }
         __builtin_amdgcn_sched_barrier(0);
       }
