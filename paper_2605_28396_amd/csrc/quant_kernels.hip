@@ -13,27 +13,107 @@ struct QuantArgs {
   int8_t* q; float* scale; int32_t* row_status;
 };
 
-// 127 x / a to the nearest integer, ties to even, as in exact arithmetic.  per_a = 127 / a rounded: the fp32 quotient is
-// off by up to 127 * 2^-23 = 1.5e-5; within twice that of a half, the quotient in 64 bits decides (127 x is exact there, and a quotient
-// that is no tie is at least 2^-41 away from one, relative, while the division rounds by 2^-53).
-__device__ __forceinline__ int quantised(float x, float per_a, float a) {
-  const float t = x * per_a, r = rintf(t);
-  if (fabsf(fabsf(t - r) - 0.5f) > 3.0e-5f) return (int)r;
-  return (int)rint((double)x * 127.0 / (double)a);
+// Eight entries of a row, raw: one vector of bf16, two of fp32.
+template <typename T>
+struct Eight {
+  static constexpr int kVecs = (int)sizeof(T) / 2;
+  u32x4 v[kVecs];
+  __device__ __forceinline__ void load(const T* x) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) v[i] = ((const u32x4*)x)[i];
+  }
+  // entries [0, n) of rows at any address, zeros behind them
+  __device__ __forceinline__ void load_some(const T* x, int n) {
+    uint32_t w[4 * kVecs] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) {
+        if constexpr (sizeof(T) == 2) w[e >> 1] |= (uint32_t)x[e] << (16 * (e & 1));
+        else w[e] = __float_as_uint(x[e]);
+      }
+#pragma unroll
+    for (int i = 0; i < 4 * kVecs; ++i) v[i >> 2][i & 3] = w[i];
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) v[i] = u32x4{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ float entry(int e) const {
+    if constexpr (sizeof(T) == 2) return e & 1 ? bf16_hi(v[0][e >> 1]) : bf16_lo(v[0][e >> 1]);
+    else return __uint_as_float(v[e >> 2][e & 3]);
+  }
+  // the larger of `top` and the magnitudes, as bits: a NaN counts as larger than inf
+  __device__ __forceinline__ uint32_t largest(uint32_t top) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t b = __float_as_uint(entry(e)) & 0x7fffffffu;
+      top = b > top ? b : top;
+    }
+    return top;
+  }
+};
+
+// Integers of eight entries: 127 x / a to the nearest, ties to even, as in exact arithmetic.  t = x (127 / a) in fp32 is off
+// by up to 127 * 2^-23 = 1.5e-5; where one lies within twice that of a half, quotients in 64 bits decide (127 x is exact there,
+// and one that is no tie is at least 2^-41 away from it, relative, while the division rounds by 2^-53).  Adding
+// 1.5 * 2^23 rounds t to a whole number, whose low byte is the sum's.
+template <typename T>
+__device__ __forceinline__ uint2 quantised(const Eight<T>& x, float per_a, float a, bool tiny) {
+  constexpr float kWhole = 12582912.f;
+  uint32_t b[8];
+  float worst = tiny ? 1.f : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float t = x.entry(e) * per_a, r = t + kWhole;
+    b[e] = __float_as_uint(r);
+    worst = fmaxf(worst, fabsf(t - (r - kWhole)));
+  }
+  if (worst > 0.5f - 3.0e-5f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = (uint32_t)(int)rint((double)x.entry(e) * 127.0 / (double)a);
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u), 0x05040100u);
+  return make_uint2(w[0], w[1]);
 }
 
-// One wave per row, twice over it: largest magnitude (as bits, so that a NaN counts as larger than inf), then the integers,
-// 8 to a lane and step.
-template <typename T>
+// One wave per row, eight entries to a lane and group.  Up to 4096 entries the row stays in registers between the search for
+// its largest magnitude and the integers; a longer one is read twice.  WHOLE: rows of whole groups that begin at multiples of
+// 16 bytes.  What bounds it is the memory.
+constexpr int kHeld = 8;                       // groups of a lane that are held
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs p) {
   const int lane = threadIdx.x & 63;
   const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= p.N) return;
   const T* x = (const T*)p.x + n * p.ld;
+  const int groups = (p.H + 7) / 8;
+  auto load = [&](Eight<T>& v, int g) __attribute__((always_inline)) {
+    if constexpr (WHOLE) {
+      v.load(x + 8 * (g < groups ? g : groups - 1));   // straight-line loads: beyond the row its last group again
+      if (g >= groups) v.clear();
+    } else {
+      v.load_some(x + 8 * g, p.H - 8 * g);
+    }
+  };
+  Eight<T> v[kHeld];
   uint32_t top = 0;
-  for (int j = lane; j < p.H; j += 64) {
-    const uint32_t b = __float_as_uint(Entry<T>::one(x + j)) & 0x7fffffffu;
-    top = b > top ? b : top;
+  const bool held = groups <= 64 * kHeld;
+  for (int g0 = 0; g0 < groups; g0 += 64 * kHeld) {
+    if (held && groups <= 64 * kHeld / 2) {
+#pragma unroll
+      for (int i = 0; i < kHeld / 2; ++i) load(v[i], lane + 64 * i);
+#pragma unroll
+      for (int i = kHeld / 2; i < kHeld; ++i) v[i].clear();
+    } else {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) load(v[i], g0 + lane + 64 * i);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) top = v[i].largest(top);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
@@ -49,19 +129,16 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs p) {
   const bool tiny = a < 1.0e-35f;                // 127 / a may overflow
   const float per_a = a > 0.f && !tiny ? 127.f / a : 0.f;
   uint2* q = (uint2*)(p.q + n * p.pitch);
-  for (int g = lane; g < p.pitch / 8; g += 64) {
-    uint32_t w[2] = {0, 0};
+  const int out = p.pitch / 8;
+  for (int g0 = 0; g0 < out; g0 += 64 * kHeld) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = 8 * g + e;
-      int v = 0;
-      if (j < p.H && a > 0.f) {
-        const float xj = Entry<T>::one(x + j);
-        v = tiny ? (int)rint((double)xj * 127.0 / (double)a) : quantised(xj, per_a, a);
+    for (int i = 0; i < kHeld; ++i) {
+      const int g = g0 + lane + 64 * i;
+      if (g < out) {
+        if (!held) load(v[i], g);
+        q[g] = a > 0.f ? quantised(v[i], per_a, a, tiny) : make_uint2(0, 0);
       }
-      w[e >> 2] |= (uint32_t)(v & 255) << (8 * (e & 3));
     }
-    q[g] = make_uint2(w[0], w[1]);
   }
 }
 
@@ -386,6 +463,130 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads that nobody reads may still be writing the LDS
 }
 
+// ---------------------------------------------------------------------------------------
+// The product, few tokens: every line of W is read once, and what bounds it is that read.
+// A workgroup to a compute unit has the tokens' integers in its LDS, in the order of the fragments of
+// v_mfma_i32_16x16x64_i8 (lane l: row l % 16 of either operand, 16 bytes of k of quarter l / 16; result e of lane l is row
+// 4 (l / 16) + e of A and row l % 16 of B), and its 8 waves walk groups of 16 entries of the head, whose
+// rows come straight from memory into the registers: a line (128 bytes of k) of 16 rows is two loads of a lane, and kAhead lines
+// are under way, over the ends of groups as well.  Waves of a workgroup take its groups in turn, so that the lines of z are
+// completed at about the same time.
+// ---------------------------------------------------------------------------------------
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
+constexpr int kAhead = 8;
+constexpr int kFewGroups = 128;                        // most groups of a workgroup: their scales are in the LDS too
+constexpr int kFewLds = 160 * 1024;
+__host__ __device__ constexpr int few_lds(int n, int pitch) { return n * 16 * pitch + kFewGroups * 16 * 4; }
+
+template <typename T, int NT, bool PAST>
+__global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (p.V + 15) / 16;
+  const int g0 = (int)((int64_t)groups * blockIdx.x / gridDim.x), g1 = (int)((int64_t)groups * (blockIdx.x + 1) / gridDim.x);
+  const int nk = p.pitch / 128;
+  const int mine = (g1 - g0 - wave + kFewWaves - 1) / kFewWaves;      // groups of this wave
+  const int total = mine > 0 ? mine * nk : 0;                        // lines
+
+  // W: the lane's bytes of line k of group g
+  int ahead_g = g0 + wave, ahead_k = 0, asked = 0;
+  const char* src = nullptr;
+  auto begin_group = [&](int g) {
+    const int64_t v = (int64_t)g * 16 + (lane & 15);
+    src = (const char*)p.W + (v < p.V ? v : p.V - 1) * p.pitch + (lane >> 4) * 16;      // rows beyond V repeat the last one
+  };
+  i32x4 w[kAhead][2];
+  auto ask = [&](int j) __attribute__((always_inline)) {
+    const i32x4* q = (const i32x4*)src;
+    if constexpr (PAST) {
+      w[j][0] = __builtin_nontemporal_load(q);
+      w[j][1] = __builtin_nontemporal_load(q + 4);
+    } else {
+      w[j][0] = q[0];
+      w[j][1] = q[4];
+    }
+    // the wave's last line is asked for again instead of one beyond it
+    if (++asked < total) {
+      src += 128;
+      if (++ahead_k == nk) {
+        ahead_k = 0;
+        ahead_g += kFewWaves;
+        begin_group(ahead_g);
+      }
+    }
+  };
+  if (total > 0) {
+    begin_group(ahead_g);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) ask(j);
+  }
+
+  // the tokens: 16 bytes of lane l of fragment (k64, n) at 16 (64 (k64 NT + n) + l).  Rows beyond T are left as they are:
+  // they enter results that are not stored.
+  for (int q = threadIdx.x; q < NT * p.pitch; q += kFewThreads) {
+    const int l = q & 63, f = q >> 6, n = f % NT, k = f / NT;
+    const int64_t t = n * 16 + (l & 15);
+    if (t < p.T) *(i32x4*)(lds + (int64_t)q * 16) = *(const i32x4*)(p.h + t * p.pitch + k * 64 + (l >> 4) * 16);
+  }
+  float* scales = (float*)(lds + NT * 16 * p.pitch);
+  for (int q = threadIdx.x; q < (g1 - g0) * 16; q += kFewThreads) {
+    const int64_t v = (int64_t)g0 * 16 + q;
+    scales[q] = p.W_scale[v < p.V ? v : p.V - 1];
+  }
+  float sh[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int64_t t = n * 16 + (lane & 15);
+    sh[n] = p.h_scale[t < p.T ? t : p.T - 1];
+  }
+  __syncthreads();
+  if (total == 0) return;
+
+  i32x4 acc[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) acc[n] = i32x4{0, 0, 0, 0};
+  int k = 0, g = g0 + wave;
+  const char* frag = lds + lane * 16;
+  for (int at = 0; at < total; at += kAhead) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (at + j < total) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const i32x4 h0 = *(const i32x4*)(frag + n * 1024), h1 = *(const i32x4*)(frag + (NT + n) * 1024);
+          acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j][0], h0, acc[n], 0, 0, 0);
+          acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j][1], h1, acc[n], 0, 0, 0);
+        }
+        frag += 2 * NT * 1024;
+      }
+      ask(j);
+      if (at + j < total && ++k == nk) {
+        const int v = g * 16 + (lane >> 4) * 4;
+        const float4 sv = *(const float4*)(scales + (g - g0) * 16 + (lane >> 4) * 4);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int64_t t = n * 16 + (lane & 15);
+          const float y[4] = {(float)acc[n][0] * (sh[n] * sv.x), (float)acc[n][1] * (sh[n] * sv.y),
+                              (float)acc[n][2] * (sh[n] * sv.z), (float)acc[n][3] * (sh[n] * sv.w)};
+          if (t < p.T) {
+            T* z = (T*)p.z + t * p.ld_z + v;
+            if (p.whole && v + 4 <= p.V) put_entries<false>(z, y, true);
+            else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (v + e < p.V) Entry<T>::put(z + e, y[e]);
+            }
+          }
+          acc[n] = i32x4{0, 0, 0, 0};
+        }
+        k = 0;
+        g += kFewWaves;
+        frag = lds + lane * 16;
+      }
+    }
+  }
+}
+
 static int check_quant(const adwin_opd_quant_problem* p) {
   if (!p) return ADWIN_E_NULL;
   if (p->struct_bytes != sizeof(*p) || !known_dtype(p->x_dtype)) return ADWIN_E_MODE;
@@ -423,10 +624,50 @@ static int product_strips(int64_t tiles, int32_t vocab_tiles) {
   return strips;
 }
 
+// Groups of 16 tokens of the kernel for few tokens, 0 where the tiles serve the call: as many as fit the LDS, at most 4.
+static int few_tokens(int64_t T, int pitch) {
+  const int64_t n = (T + 15) / 16;
+  return n <= 4 && few_lds((int)n, pitch) <= kFewLds ? (int)n : 0;
+}
+
+template <typename T, int NT>
+static hipError_t launch_few_n(const ProductArgs& a, bool past, hipStream_t st) {
+  const int groups = (a.V + 15) / 16;
+  int blocks = (groups + kFewWaves - 1) / kFewWaves;
+  if (blocks > 256) blocks = 256;
+  if ((groups + blocks - 1) / blocks > kFewGroups) blocks = (groups + kFewGroups - 1) / kFewGroups;
+  const int bytes = few_lds(NT, a.pitch);
+  if (past) quant_few_kernel<T, NT, true><<<blocks, kFewThreads, bytes, st>>>(a);
+  else quant_few_kernel<T, NT, false><<<blocks, kFewThreads, bytes, st>>>(a);
+  return hipGetLastError();
+}
+template <typename T>
+static hipError_t launch_few(const ProductArgs& a, int n, bool past, hipStream_t st) {
+  switch (n) {
+    case 1: return launch_few_n<T, 1>(a, past, st);
+    case 2: return launch_few_n<T, 2>(a, past, st);
+    case 3: return launch_few_n<T, 3>(a, past, st);
+    default: return launch_few_n<T, 4>(a, past, st);
+  }
+}
+
 // large dynamic LDS of the product, once per device
+template <typename T, int NT>
+static hipError_t few_opt_in() {
+  for (const void* k : {(const void*)quant_few_kernel<T, NT, false>, (const void*)quant_few_kernel<T, NT, true>}) {
+    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 hipError_t quant_kernels_opt_in() {
   for (const void* k : {(const void*)quant_tile_kernel<uint16_t>, (const void*)quant_tile_kernel<float>}) {
     const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kQLds);
+    if (e != hipSuccess) return e;
+  }
+  for (hipError_t (*set)() : {few_opt_in<uint16_t, 1>, few_opt_in<uint16_t, 2>, few_opt_in<uint16_t, 3>, few_opt_in<uint16_t, 4>,
+                              few_opt_in<float, 1>, few_opt_in<float, 2>, few_opt_in<float, 3>, few_opt_in<float, 4>}) {
+    const hipError_t e = set();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -435,8 +676,15 @@ static hipError_t quant_opt_in() { return first_use_on_device(2) ? quant_kernels
 
 static hipError_t launch_quant_rows(const QuantArgs& a, int32_t dtype, hipStream_t st) {
   const unsigned blocks = (unsigned)((a.N + 3) / 4);
-  if (dtype == ADWIN_DT_BF16) quant_rows_kernel<uint16_t><<<blocks, 256, 0, st>>>(a);
-  else quant_rows_kernel<float><<<blocks, 256, 0, st>>>(a);
+  const int64_t size = dtype == ADWIN_DT_BF16 ? 2 : 4;
+  const bool whole = ((uintptr_t)a.x & 15) == 0 && ((a.ld * size) & 15) == 0 && (a.H & 7) == 0;
+  if (dtype == ADWIN_DT_BF16) {
+    if (whole) quant_rows_kernel<uint16_t, true><<<blocks, 256, 0, st>>>(a);
+    else quant_rows_kernel<uint16_t, false><<<blocks, 256, 0, st>>>(a);
+  } else {
+    if (whole) quant_rows_kernel<float, true><<<blocks, 256, 0, st>>>(a);
+    else quant_rows_kernel<float, false><<<blocks, 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -483,6 +731,13 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
   a.pitch = ADWIN_QUANT_PITCH(p->H);
   const int64_t size = p->z_dtype == ADWIN_DT_BF16 ? 2 : 4;
   a.whole = ((uintptr_t)p->z & 15) == 0 && (p->ld_z * size & 15) == 0;
+  ADWIN_HIP_TRY(quant_opt_in());
+  const int few = few_tokens(p->T, a.pitch);
+  if (few > 0) {
+    const bool past = (int64_t)p->V * a.pitch > ((int64_t)320 << 20);
+    ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_few<uint16_t>(a, few, past, stream) : launch_few<float>(a, few, past, stream));
+    return ADWIN_OK;
+  }
   const int64_t tiles = (p->T + kQTile - 1) / kQTile;
   a.token_tiles = (int32_t)tiles;
   a.vocab_tiles = (p->V + kQTile - 1) / kQTile;
@@ -490,7 +745,6 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
   a.group = 4;
   if (tiles * a.strips >= kMaxRows) return ADWIN_E_SHAPE;
   const unsigned blocks = (unsigned)(tiles * a.strips);
-  ADWIN_HIP_TRY(quant_opt_in());
   if (p->z_dtype == ADWIN_DT_BF16) quant_tile_kernel<uint16_t><<<blocks, 256, kQLds, stream>>>(a);
   else quant_tile_kernel<float><<<blocks, 256, kQLds, stream>>>(a);
   ADWIN_HIP_TRY(hipGetLastError());
