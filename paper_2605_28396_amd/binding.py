@@ -515,15 +515,18 @@ def adwin_opd_quant_logits_workspace_bytes(p: adwin_opd_quant_logits_problem) ->
 @_on_stream
 def adwin_opd_quant_logits(h, W_q, W_scale, z_dtype=ADWIN_DT_BF16, z=None, row_status=False) -> dict:
     """Logits `z` [T, V] of hidden states h [T, H] under the head that adwin_opd_quant_rows made of W [V, H].  z: where
-    they go (else a new tensor)."""
+    they go; else a new tensor, whose rows begin at multiples of 16 bytes (those of a contiguous one may not, and are
+    written entry by entry then)."""
     ld = _rows("h", h)
     T, H = h.shape
     V = W_q.shape[0]
     W_ptr = _flat("W_q", W_q, torch.int8, V, ADWIN_QUANT_PITCH(H))
     s_ptr = _flat("W_scale", W_scale, torch.float32, V)
     if z is None:
-        z = torch.empty(T, V, dtype=_TORCH_DTYPE[z_dtype], device=h.device)
-        ld_z = V
+        ld_z = (V + 7) & ~7
+        z = torch.empty(T, ld_z, dtype=_TORCH_DTYPE[z_dtype], device=h.device)
+        if ld_z != V:
+            z = z[:, :V]
     else:
         ld_z = _rows("z", z)
         z_dtype = _DTYPE[z.dtype]

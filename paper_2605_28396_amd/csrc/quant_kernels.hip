@@ -475,10 +475,9 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
 constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
 constexpr int kAhead = 8;
 constexpr int kFewGroups = 128;                        // most groups of a workgroup: their scales are in the LDS too
-constexpr int kFewLds = 160 * 1024;
 __host__ __device__ constexpr int few_lds(int n, int pitch) { return n * 16 * pitch + kFewGroups * 16 * 4; }
 
-template <typename T, int NT, bool PAST>
+template <typename T, int NT>
 __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -489,56 +488,64 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
   const int total = mine > 0 ? mine * nk : 0;                        // lines
 
   // W: the lane's bytes of line k of group g
+  const int turn = (int)((blockIdx.x * kFewWaves + wave) % (uint32_t)nk);    // the line that the wave begins with
   int ahead_g = g0 + wave, ahead_k = 0, asked = 0;
   const char* src = nullptr;
   auto begin_group = [&](int g) {
     const int64_t v = (int64_t)g * 16 + (lane & 15);
-    src = (const char*)p.W + (v < p.V ? v : p.V - 1) * p.pitch + (lane >> 4) * 16;      // rows beyond V repeat the last one
+    src = (const char*)p.W + (v < p.V ? v : p.V - 1) * p.pitch + turn * 128 + (lane >> 4) * 16;   // rows beyond V repeat the last one
   };
   i32x4 w[kAhead][2];
   auto ask = [&](int j) __attribute__((always_inline)) {
     const i32x4* q = (const i32x4*)src;
-    if constexpr (PAST) {
-      w[j][0] = __builtin_nontemporal_load(q);
-      w[j][1] = __builtin_nontemporal_load(q + 4);
-    } else {
-      w[j][0] = q[0];
-      w[j][1] = q[4];
-    }
+    w[j][0] = q[0];
+    w[j][1] = q[4];
     // the wave's last line is asked for again instead of one beyond it
     if (++asked < total) {
       src += 128;
-      if (++ahead_k == nk) {
+      if (++ahead_k == nk - turn) src -= p.pitch;
+      if (ahead_k == nk) {
         ahead_k = 0;
         ahead_g += kFewWaves;
         begin_group(ahead_g);
       }
     }
   };
-  if (total > 0) {
-    begin_group(ahead_g);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) ask(j);
-  }
-
-  // the tokens: 16 bytes of lane l of fragment (k64, n) at 16 (64 (k64 NT + n) + l).  Rows beyond T are left as they are:
-  // they enter results that are not stored.
-  for (int q = threadIdx.x; q < NT * p.pitch; q += kFewThreads) {
-    const int l = q & 63, f = q >> 6, n = f % NT, k = f / NT;
-    const int64_t t = n * 16 + (l & 15);
-    if (t < p.T) *(i32x4*)(lds + (int64_t)q * 16) = *(const i32x4*)(p.h + t * p.pitch + k * 64 + (l >> 4) * 16);
-  }
   float* scales = (float*)(lds + NT * 16 * p.pitch);
-  for (int q = threadIdx.x; q < (g1 - g0) * 16; q += kFewThreads) {
-    const int64_t v = (int64_t)g0 * 16 + q;
-    scales[q] = p.W_scale[v < p.V ? v : p.V - 1];
-  }
-  float sh[NT];
+  float sh[NT], sw[kFewGroups * 16 / kFewThreads];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int64_t t = n * 16 + (lane & 15);
     sh[n] = p.h_scale[t < p.T ? t : p.T - 1];
   }
+#pragma unroll
+  for (int i = 0; i < kFewGroups * 16 / kFewThreads; ++i) {
+    const int q = i * kFewThreads + threadIdx.x;
+    const int64_t v = (int64_t)g0 * 16 + (q < (g1 - g0) * 16 ? q : 0);
+    sw[i] = p.W_scale[v < p.V ? v : p.V - 1];
+  }
+  // the tokens: fragment (k64, n) at 1024 (k64 NT + n), by direct loads.  Rows beyond T repeat the last one; they enter
+  // results that are not stored.
+  uint32_t from[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int64_t t = n * 16 + (lane & 15);
+    from[n] = (uint32_t)(t < p.T ? t : p.T - 1) * (uint32_t)p.pitch + (lane >> 4) * 16u;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  for (int k = wave; k < 2 * nk; k += kFewWaves)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) dma16_at<0>(lds0 + (uint32_t)(k * NT + n) * 1024u, from[n], (const char*)p.h + k * 64);
+  if (total > 0) {
+    begin_group(ahead_g);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) ask(j);
+  }
+#pragma unroll
+  for (int i = 0; i < kFewGroups * 16 / kFewThreads; ++i) scales[i * kFewThreads + threadIdx.x] = sw[i];
+  // loads return in order: the tokens are there when no more than the lines that were asked for behind them are under way
+  if (total > 0) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * kAhead) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (total == 0) return;
 
@@ -546,7 +553,7 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n] = i32x4{0, 0, 0, 0};
   int k = 0, g = g0 + wave;
-  const char* frag = lds + lane * 16;
+  const char* frag = lds + lane * 16 + turn * (2 * NT * 1024);
   for (int at = 0; at < total; at += kAhead) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -560,7 +567,8 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
         frag += 2 * NT * 1024;
       }
       ask(j);
-      if (at + j < total && ++k == nk) {
+      if (at + j < total && ++k == nk - turn) frag = lds + lane * 16;
+      if (at + j < total && k == nk) {
         const int v = g * 16 + (lane >> 4) * 4;
         const float4 sv = *(const float4*)(scales + (g - g0) * 16 + (lane >> 4) * 4);
 #pragma unroll
@@ -581,7 +589,7 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
         }
         k = 0;
         g += kFewWaves;
-        frag = lds + lane * 16;
+        frag = lds + lane * 16 + turn * (2 * NT * 1024);
       }
     }
   }
@@ -627,47 +635,36 @@ static int product_strips(int64_t tiles, int32_t vocab_tiles) {
 // Groups of 16 tokens of the kernel for few tokens, 0 where the tiles serve the call: as many as fit the LDS, at most 4.
 static int few_tokens(int64_t T, int pitch) {
   const int64_t n = (T + 15) / 16;
-  return n <= 4 && few_lds((int)n, pitch) <= kFewLds ? (int)n : 0;
+  return n <= 4 && few_lds((int)n, pitch) <= kQLds ? (int)n : 0;
 }
 
 template <typename T, int NT>
-static hipError_t launch_few_n(const ProductArgs& a, bool past, hipStream_t st) {
+static hipError_t launch_few_n(const ProductArgs& a, hipStream_t st) {
   const int groups = (a.V + 15) / 16;
   int blocks = (groups + kFewWaves - 1) / kFewWaves;
   if (blocks > 256) blocks = 256;
   if ((groups + blocks - 1) / blocks > kFewGroups) blocks = (groups + kFewGroups - 1) / kFewGroups;
-  const int bytes = few_lds(NT, a.pitch);
-  if (past) quant_few_kernel<T, NT, true><<<blocks, kFewThreads, bytes, st>>>(a);
-  else quant_few_kernel<T, NT, false><<<blocks, kFewThreads, bytes, st>>>(a);
+  quant_few_kernel<T, NT><<<blocks, kFewThreads, few_lds(NT, a.pitch), st>>>(a);
   return hipGetLastError();
 }
 template <typename T>
-static hipError_t launch_few(const ProductArgs& a, int n, bool past, hipStream_t st) {
+static hipError_t launch_few(const ProductArgs& a, int n, hipStream_t st) {
   switch (n) {
-    case 1: return launch_few_n<T, 1>(a, past, st);
-    case 2: return launch_few_n<T, 2>(a, past, st);
-    case 3: return launch_few_n<T, 3>(a, past, st);
-    default: return launch_few_n<T, 4>(a, past, st);
+    case 1: return launch_few_n<T, 1>(a, st);
+    case 2: return launch_few_n<T, 2>(a, st);
+    case 3: return launch_few_n<T, 3>(a, st);
+    default: return launch_few_n<T, 4>(a, st);
   }
 }
 
 // large dynamic LDS of the product, once per device
-template <typename T, int NT>
-static hipError_t few_opt_in() {
-  for (const void* k : {(const void*)quant_few_kernel<T, NT, false>, (const void*)quant_few_kernel<T, NT, true>}) {
-    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
 hipError_t quant_kernels_opt_in() {
-  for (const void* k : {(const void*)quant_tile_kernel<uint16_t>, (const void*)quant_tile_kernel<float>}) {
+  for (const void* k : {(const void*)quant_tile_kernel<uint16_t>, (const void*)quant_tile_kernel<float>,
+                        (const void*)quant_few_kernel<uint16_t, 1>, (const void*)quant_few_kernel<uint16_t, 2>,
+                        (const void*)quant_few_kernel<uint16_t, 3>, (const void*)quant_few_kernel<uint16_t, 4>,
+                        (const void*)quant_few_kernel<float, 1>, (const void*)quant_few_kernel<float, 2>,
+                        (const void*)quant_few_kernel<float, 3>, (const void*)quant_few_kernel<float, 4>}) {
     const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kQLds);
-    if (e != hipSuccess) return e;
-  }
-  for (hipError_t (*set)() : {few_opt_in<uint16_t, 1>, few_opt_in<uint16_t, 2>, few_opt_in<uint16_t, 3>, few_opt_in<uint16_t, 4>,
-                              few_opt_in<float, 1>, few_opt_in<float, 2>, few_opt_in<float, 3>, few_opt_in<float, 4>}) {
-    const hipError_t e = set();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -734,8 +731,7 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
   ADWIN_HIP_TRY(quant_opt_in());
   const int few = few_tokens(p->T, a.pitch);
   if (few > 0) {
-    const bool past = (int64_t)p->V * a.pitch > ((int64_t)320 << 20);
-    ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_few<uint16_t>(a, few, past, stream) : launch_few<float>(a, few, past, stream));
+    ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_few<uint16_t>(a, few, stream) : launch_few<float>(a, few, stream));
     return ADWIN_OK;
   }
   const int64_t tiles = (p->T + kQTile - 1) / kQTile;
