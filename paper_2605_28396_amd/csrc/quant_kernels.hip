@@ -467,13 +467,13 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
 // The product, few tokens: every line of W is read once, and what bounds it is that read.
 // A workgroup to a compute unit has the tokens' integers in its LDS, in the order of the fragments of
 // v_mfma_i32_16x16x64_i8 (lane l: row l % 16 of either operand, 16 bytes of k of quarter l / 16; result e of lane l is row
-// 4 (l / 16) + e of A and row l % 16 of B), and its 8 waves walk groups of 16 entries of the head, whose
+// 4 (l / 16) + e of A and row l % 16 of B), and its 16 waves walk groups of 16 entries of the head, whose
 // rows come straight from memory into the registers: a line (128 bytes of k) of 16 rows is two loads of a lane, and kAhead lines
 // are under way, over the ends of groups as well.  Waves of a workgroup take its groups in turn, so that the lines of z are
 // completed at about the same time.
 // ---------------------------------------------------------------------------------------
-constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
-constexpr int kAhead = 8;
+constexpr int kFewThreads = 1024, kFewWaves = kFewThreads / 64;
+constexpr int kAhead = 4;
 constexpr int kFewGroups = 128;                        // most groups of a workgroup: their scales are in the LDS too
 __host__ __device__ constexpr int few_lds(int n, int pitch) { return n * 16 * pitch + kFewGroups * 16 * 4; }
 
