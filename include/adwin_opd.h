@@ -471,8 +471,8 @@ int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, void* worksp
  *   (beyond V of them: -1 and 0).
  * z may hold -inf (a masked entry: probability 0, it takes no part in the entropy; its
  * log-probability is -inf where it is asked for).  An id < 0 is not scored (logp 0); an id >= V is not either and sets
- * ADWIN_DEV_BAD_ID.  A row of which no id is scored is not read: zeros, -1 in top_ids (rows outside a window
- * are given so).  With G = 0 every row is computed.  A row with a NaN or +inf, or of nothing but -inf,
+ * ADWIN_DEV_BAD_ID.  A row of which no id is scored is not computed: zeros, -1 in top_ids (rows outside a
+ * window are given so).  With G = 0 every row is computed.  A row with a NaN or +inf, or of nothing but -inf,
  * is excluded with ADWIN_DEV_NONFINITE.
  * Limits: 0 <= T < 2^31, 1 <= V <= 2^28, 0 <= G <= ADWIN_MAX_GIVEN, 0 <= top <= ADWIN_MAX_TOP. */
 typedef struct adwin_opd_logp_problem {
@@ -487,7 +487,7 @@ typedef struct adwin_opd_logp_problem {
   /* device outputs; NULL = not wanted */
   float*   logp;             /* [T, G]                                                         */
   float*   entropy;          /* [T]                                                            */
-  float*   norm;             /* [T, 2] m and s: what the gradient needs of this call; 0, 0 where excluded or not read */
+  float*   norm;             /* [T, 2] m and s: what the gradient needs of this call; 0, 0 where excluded or not computed */
   int32_t* top_ids;          /* [T, top]                                                       */
   float*   top_logp;         /* [T, top]                                                       */
   int32_t* row_status;       /* [T] ADWIN_DEV_* bits                                           */

@@ -351,42 +351,41 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
   const int tid = threadIdx.x;
   const int64_t r = blockIdx.x / (uint32_t)a.pieces;
   const int piece = (int)(blockIdx.x - (uint32_t)r * (uint32_t)a.pieces);
+  const Piece<T> p((const T*)a.z + r * a.ld, a.V, piece, a.pieces);
+  const int last = p.v1 - tid;                      // a thread's vectors: p.v0 + tid + 256 k below p.v1
+  // whole steps, whose loads stand in no branch: the wait for a vector then leaves the younger ones in flight
+  const int whole = (p.v1 - p.v0) / (kStep * kThreads);
+  int i0 = p.v0;
+  uint4 v[kStep];
+  auto load = [&](int u) { v[u] = p.row.template vec<PAST>(i0 + tid + kThreads * u); };
+  auto load_any = [&](int u) {
+    v[u] = Entry<T>::none();
+    if (i0 + kThreads * u < last) load(u);
+  };
+  // the first vectors are under way before the ids say whether the row is computed
+  if (whole > 0) {
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) load(u);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) load_any(u);
+  }
   const RowIds is = row_ids(a.ids, a.G, a.V, r);
   Sums sum = no_sums();
   float given = 0.f;
   bool scored = false;
   if (is.live) {
-    const Piece<T> p((const T*)a.z + r * a.ld, a.V, piece, a.pieces);
     float bound = INFINITY;
     if (tid == 0) l.count = 0;
     float edge[1] = {-INFINITY};
-    if (tid < p.edge) {
-      edge[0] = Entry<T>::one(p.row.p + p.row.edge_index(tid));
-      add_entries(sum, edge, a.c);
-    }
-    const int last = p.v1 - tid;                    // a thread's vectors: p.v0 + tid + 256 k below p.v1
-    // whole steps, whose loads stand in no branch: the wait for a vector then leaves the younger ones in flight
-    const int whole = (p.v1 - p.v0) / (kStep * kThreads);
-    int i0 = p.v0;
-    uint4 v[kStep];
-    auto load = [&](int u) { v[u] = p.row.template vec<PAST>(i0 + tid + kThreads * u); };
-    auto load_any = [&](int u) {
-      v[u] = Entry<T>::none();
-      if (i0 + kThreads * u < last) load(u);
-    };
+    if (tid < p.edge) edge[0] = Entry<T>::one(p.row.p + p.row.edge_index(tid));
+    if (a.pieces == 1) given = given_logit<T>(a, r, &scored);
     auto add = [&](int u) {
       float x[N];
       Entry<T>::unpack(v[u], x);
       return add_entries(sum, x, a.c);
     };
-    if (whole > 0) {
-#pragma unroll
-      for (int u = 0; u < kStep; ++u) load(u);
-    } else {
-#pragma unroll
-      for (int u = 0; u < kStep; ++u) load_any(u);
-    }
-    if (a.pieces == 1) given = given_logit<T>(a, r, &scored);
+    if (tid < p.edge) add_entries(sum, edge, a.c);
     // the first vectors, which give the first bound and are then gone through again
 #pragma unroll
     for (int u = 0; u < kStep; ++u) add(u);
@@ -441,9 +440,16 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       }
     }
     if (a.top > 0) {
-      __syncthreads();                              // all have read the first bound
-      l.most[tid] = order_bits(sum.m) >> 16;
-      if (!select_found(l, a.top)) select_slowly(p, a.top, l);
+      __syncthreads();                              // all have read the first bound, and listed what reaches it
+      bool listed = true;
+      if (whole == 0) {                             // there has been no later one
+        listed = l.count <= kFound;
+        if (listed) rank_found(l, l.count, a.top);
+      } else {
+        l.most[tid] = order_bits(sum.m) >> 16;
+        listed = select_found(l, a.top);
+      }
+      if (!listed) select_slowly(p, a.top, l);
     }
     sum = piece_sums(p, sum, a.c, part);
   }
@@ -465,7 +471,7 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
   __shared__ Select l;
   const int64_t r = blockIdx.x;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
   const RowIds is = row_ids(a.ids, a.G, a.V, r);
   Sums sum = no_sums();
   float given = 0.f;
@@ -479,8 +485,11 @@ __global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
       constexpr int kMine = kMaxPieces * ADWIN_MAX_TOP / kThreads;
       uint64_t key[kMine], most = 0;
 #pragma unroll
+      for (int u = 0; u < kMine; ++u)               // straight-line loads: beyond the last the last again
+        if (u * kThreads < n) key[u] = keys[u * kThreads + tid < n ? u * kThreads + tid : n - 1];
+#pragma unroll
       for (int u = 0; u < kMine; ++u) {
-        key[u] = u * kThreads + tid < n ? keys[u * kThreads + tid] : 0;
+        if (u * kThreads + tid >= n) key[u] = 0;
         most = key[u] > most ? key[u] : most;
       }
       if (tid == 0) l.count = 0;
@@ -505,25 +514,25 @@ __global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
         }
       }
     }
-    sum.m = -INFINITY;
-    for (int i = 0; i < a.pieces; ++i) sum.m = fmaxf(sum.m, part[i].x);
-    sum.s = sum.t = 0.f;
-    for (int i = 0; i < a.pieces; ++i) {
-      const float4 q = part[i];
-      const float by = (q.x - sum.m) * a.c, f = fast_exp2(by);
-      sum.t = fmaf(f, fmaf(q.y, fmaxf(by, kNegBig), q.z), sum.t);
-      sum.s = fmaf(f, q.y, sum.s);
-    }
+    // every wave by itself, a piece to a lane
+    float4 q = part[lane < a.pieces ? lane : 0];
+    if (lane >= a.pieces) q = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    sum.m = wave_max(q.x);
+    const float by = (q.x - sum.m) * a.c, f = fast_exp2(by);
+    sum.s = wave_sum(f * q.y);
+    sum.t = wave_sum(f * fmaf(q.y, fmaxf(by, kNegBig), q.z));
     __syncthreads();
   }
   finish_row(a, r, sum, l.kept, is, given, scored);
 }
 
-// Pieces of a row.  One for calls of many rows; few rows are cut so that there are 1,024 workgroups (four to a compute
-// unit), each with a step of its threads or more.
+// Pieces of a row.  One for calls of 256 rows or more; fewer are cut so that every compute unit has a workgroup, each with half a
+// step of its threads or more.  us, target of 256 / 512 / 1,024 workgroups, bf16, V = 151,936: 64 rows 23.8 / 22.1 / 22.8, 300 rows
+// 42 / 42 / 39, 500 rows 48 / 51 / 53, 1,000 rows 76 / 73 / 87; fp32, V = 32,771: 100 rows 23.4 / 21.9 / 21.7, 400 rows 26 / 31 / 31,
+// 1,000 rows 35 / 35 / 49 (one piece to a row: 1 row 31 us, in pieces 20).
 static int logp_pieces(int64_t T, int32_t V, int32_t dtype) {
   const int64_t step = (int64_t)kStep * kThreads * (dtype == ADWIN_DT_BF16 ? 8 : 4) / 2;
-  int64_t n = (1024 + T - 1) / (T > 0 ? T : 1);
+  int64_t n = (256 + T - 1) / (T > 0 ? T : 1);
   if (n > V / step) n = V / step;
   return (int)(n < 1 ? 1 : n > kMaxPieces ? kMaxPieces : n);
 }
