@@ -115,14 +115,18 @@ struct Piece {
   }
 };
 
-constexpr int kFound = 1536;       // keys that a workgroup can list: 1,100 pass the first bound at top = 64 and V = 151,936
+constexpr int kPart = 384;         // keys that a wave can list: some 90 pass the bounds at top = 64 and V = 151,936
+constexpr int kFound = kWaves * kPart;
+constexpr int kDense = 512;        // ... and that can be ranked
 
 struct Select {                    // in the LDS
   uint64_t kept[ADWIN_MAX_TOP];    // the result: sorted, zeros behind the last
   uint64_t found[kFound];
+  uint64_t dense[kDense];
   uint64_t best[kThreads + 1];
   uint32_t most[kThreads];         // the threads' largest entries, as order_bits >> 16
-  int count, chosen;
+  int listed[kWaves];
+  int count;
 };
 
 // A lower bound of the `top`-th largest of the 256 numbers in `most`, exact in 16 bits, by every wave: the bits from the
@@ -150,12 +154,12 @@ __device__ __forceinline__ float bound_value(uint32_t at) {
   return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 
-// found[0, n): the `top` largest of them into `kept`, by counting the larger ones.  Keys differ.
-__device__ __forceinline__ void rank_found(Select& l, int n, int top) {
+// keys[0, n): the `top` largest of them into `kept`, by counting the larger ones.  Keys differ.
+__device__ __forceinline__ void rank_keys(Select& l, const uint64_t* keys, int n, int top) {
   for (int q = threadIdx.x; q < n; q += kThreads) {
-    const uint64_t v = l.found[q];
+    const uint64_t v = keys[q];
     int r = 0;
-    for (int j = 0; j < n; ++j) r += l.found[j] > v;
+    for (int j = 0; j < n; ++j) r += keys[j] > v;
     if (r < top) l.kept[r] = v;
   }
   if ((int)threadIdx.x >= n && (int)threadIdx.x < top) l.kept[threadIdx.x] = 0;
@@ -205,7 +209,7 @@ __device__ __forceinline__ void select_slowly(const Piece<T>& p, int top, Select
     const int n = l.count;
     if (tid < have) l.found[n + tid] = l.found[kFound - 1 - tid];
     __syncthreads();
-    rank_found(l, n + have, top);
+    rank_keys(l, l.found, n + have, top);
     have = have + n < top ? have + n : top;
     __syncthreads();
   }
@@ -213,54 +217,59 @@ __device__ __forceinline__ void select_slowly(const Piece<T>& p, int top, Select
   __syncthreads();
 }
 
-// What of `found` reaches the bound of the threads' largest entries, ranked.  Every thread has written its `most`.
-// False where more was found than could be listed.
-__device__ __forceinline__ bool select_found(Select& l, int top) {
+// What the waves have listed (`listed` keys of this one) and reaches the bound of the threads' largest entries, ranked.  Every
+// thread has written its `most`.  False where more was found than could be listed or can be ranked.
+__device__ __forceinline__ bool select_found(Select& l, int listed, int top) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane == 0) l.listed[wave] = listed;
+  if (threadIdx.x == 0) l.count = 0;
   __syncthreads();
-  const int n = l.count;
-  if (n > kFound) return false;
+  bool fits = true;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) fits = fits && l.listed[w] <= kPart;
+  if (!fits) return false;
   const uint64_t bound = (uint64_t)wave_bound(l.most, top) << 48;
-  // compacted in place: a thread's keys are in registers before the first is written
-  uint64_t key[kFound / kThreads];
+  uint64_t key[kPart / 64];
+  int n = 0;
 #pragma unroll
-  for (int u = 0; u < kFound / kThreads; ++u) {
-    const int q = u * kThreads + threadIdx.x;
-    key[u] = q < n ? l.found[q] : 0;
+  for (int u = 0; u < kPart / 64; ++u) {
+    const int q = 64 * u + lane;
+    key[u] = q < listed ? l.found[wave * kPart + q] : 0;
+    if (key[u] < bound) key[u] = 0;
+    n += __popcll(__ballot(key[u] != 0));
   }
-  if (threadIdx.x == 0) l.chosen = 0;
-  __syncthreads();
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&l.count, n);
+  at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-  for (int u = 0; u < kFound / kThreads; ++u)
-    if (key[u] && key[u] >= bound) l.found[atomicAdd(&l.chosen, 1)] = key[u];
+  for (int u = 0; u < kPart / 64; ++u) {
+    const uint64_t which = __ballot(key[u] != 0);
+    const int q = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)which, 0));
+    if (key[u] && q < kDense) l.dense[q] = key[u];
+    at += __popcll(which);
+  }
   __syncthreads();
-  rank_found(l, l.chosen, top);
+  if (l.count > kDense) return false;
+  rank_keys(l, l.dense, l.count, top);
   __syncthreads();
   return true;
 }
 
-__device__ __forceinline__ void list_key(Select& l, uint64_t key) {
-  const int q = atomicAdd(&l.count, 1);
-  if (q < kFound) l.found[q] = key;
+// Lists, in the wave's part, what entry x of index i is of the lanes where `is`.  No lane waits for an answer of the LDS.
+__device__ __forceinline__ void list_entry(Select& l, int& listed, bool is, float x, int i) {
+  const uint64_t which = __ballot(is);
+  if (which == 0) return;
+  const int q = listed + __builtin_amdgcn_mbcnt_hi((uint32_t)(which >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)which, 0));
+  if (is && q < kPart) l.found[(threadIdx.x >> 6) * kPart + q] = order_key(x, i);
+  listed += __popcll(which);
 }
-// Entries of vector v that reach the bound; `first`: the index of the vector's first one.
+// Entries of vector v that reach the bound, in the lanes where `is`; `first`: the index of the vector's first one.
 template <typename T>
-__device__ __forceinline__ void list_entries(Select& l, const uint4& v, int first, float bound) {
+__device__ __forceinline__ void list_entries(Select& l, int& listed, bool is, const uint4& v, int first, float bound) {
   float x[Entry<T>::kPerVec];
   Entry<T>::unpack(v, x);
-  uint32_t which = 0;
 #pragma unroll
-  for (int e = 0; e < Entry<T>::kPerVec; ++e) which |= x[e] >= bound ? 1u << e : 0u;
-  uint32_t w0 = v.x, w1 = v.y, w2 = v.z, w3 = v.w;
-  asm("" : "+v"(w0), "+v"(w1), "+v"(w2), "+v"(w3));      // four registers, not an array that is indexed in memory
-  while (which) {
-    const int e = __ffs(which) - 1;
-    which &= which - 1;
-    const int at = e * (int)sizeof(T) / 4;
-    const uint32_t even = at & 2 ? w2 : w0, odd = at & 2 ? w3 : w1;
-    uint32_t w = at & 1 ? odd : even;
-    if constexpr (sizeof(T) == 2) w = e & 1 ? w & 0xffff0000u : w << 16;
-    list_key(l, order_key(__uint_as_float(w), first + e));
-  }
+  for (int e = 0; e < Entry<T>::kPerVec; ++e) list_entry(l, listed, is && x[e] >= bound, x[e], first + e);
 }
 
 // The sums relative to the piece's largest logit: 1 <= s, and the entropy log s - t / s has no terms larger than need be.
@@ -376,7 +385,7 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
   bool scored = false;
   if (is.live) {
     float bound = INFINITY;
-    if (tid == 0) l.count = 0;
+    int listed = 0;                                 // keys of this wave
     float edge[1] = {-INFINITY};
     if (tid < p.edge) edge[0] = Entry<T>::one(p.row.p + p.row.edge_index(tid));
     if (a.pieces == 1) given = given_logit<T>(a, r, &scored);
@@ -394,10 +403,10 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       __syncthreads();
       bound = bound_value(wave_bound(l.most, a.top));
       if (tid == 0) shared_bound = bound;
-      if (tid < p.edge && edge[0] >= bound) list_key(l, order_key(edge[0], p.row.edge_index(tid)));
+      list_entry(l, listed, tid < p.edge && edge[0] >= bound, edge[0], p.row.edge_index(tid));
 #pragma unroll
       for (int u = 0; u < kStep; ++u)
-        if (i0 + kThreads * u < last) list_entries<T>(l, v[u], p.row.index(i0 + tid + kThreads * u), bound);
+        list_entries<T>(l, listed, i0 + kThreads * u < last, v[u], p.row.index(i0 + tid + kThreads * u), bound);
     }
     i0 += kStep * kThreads;
     if (whole > 1) {
@@ -422,13 +431,13 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       if (step + 1 < whole) {
 #pragma unroll
         for (int u = 0; u < kStep; ++u) {
-          if (add(u) >= bound) list_entries<T>(l, v[u], first + kThreads * N * u, bound);
+          if (__any(add(u) >= bound)) list_entries<T>(l, listed, true, v[u], first + kThreads * N * u, bound);
           load(u);
         }
       } else {
 #pragma unroll
         for (int u = 0; u < kStep; ++u)
-          if (add(u) >= bound) list_entries<T>(l, v[u], first + kThreads * N * u, bound);
+          if (__any(add(u) >= bound)) list_entries<T>(l, listed, true, v[u], first + kThreads * N * u, bound);
       }
     }
     if (whole > 0) {
@@ -436,20 +445,14 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       for (int u = 0; u < kStep; ++u) load_any(u);
 #pragma unroll
       for (int u = 0; u < kStep; ++u) {
-        if (add(u) >= bound && i0 + kThreads * u < last) list_entries<T>(l, v[u], p.row.index(i0 + tid + kThreads * u), bound);
+        if (__any(add(u) >= bound))
+          list_entries<T>(l, listed, i0 + kThreads * u < last, v[u], p.row.index(i0 + tid + kThreads * u), bound);
       }
     }
     if (a.top > 0) {
-      __syncthreads();                              // all have read the first bound, and listed what reaches it
-      bool listed = true;
-      if (whole == 0) {                             // there has been no later one
-        listed = l.count <= kFound;
-        if (listed) rank_found(l, l.count, a.top);
-      } else {
-        l.most[tid] = order_bits(sum.m) >> 16;
-        listed = select_found(l, a.top);
-      }
-      if (!listed) select_slowly(p, a.top, l);
+      __syncthreads();                              // all have read the first bound
+      l.most[tid] = order_bits(sum.m) >> 16;
+      if (!select_found(l, listed, a.top)) select_slowly(p, a.top, l);
     }
     sum = piece_sums(p, sum, a.c, part);
   }
@@ -504,7 +507,7 @@ __global__ __launch_bounds__(kThreads) void join_logp_kernel(LogpArgs a) {
         }
       __syncthreads();
       if (l.count <= kFound) {
-        rank_found(l, l.count, a.top);
+        rank_keys(l, l.found, l.count, a.top);
       } else {                                      // ties in all pieces: every key against all others
         for (int q = tid; q < n; q += kThreads) {
           const uint64_t v = keys[q];
