@@ -88,14 +88,15 @@ const char* adwin_opd_strerror(int status) {
     case ADWIN_E_NULL: return "a required pointer is NULL";
     case ADWIN_E_SHAPE:
       return "bad shape: need B>=1, 0<=T<2^31, V a positive multiple of 8, H_s and H_t positive "
-             "multiples of 64";
+             "multiples of 64 (the token-scoring calls: sizes and pitches as their structs say)";
     case ADWIN_E_OFFSETS: return "offsets must start at 0, be non-decreasing and end at T";
     case ADWIN_E_WINDOW: return "window lengths must be >= 0";
-    case ADWIN_E_ALIGN: return "device pointers must be 16-byte aligned";
+    case ADWIN_E_ALIGN:
+      return "device pointers must be 16-byte aligned (x, h, z and dz of the token-scoring calls: to their entries)";
     case ADWIN_E_WORKSPACE: return "workspace is NULL, not 256-byte aligned or too small";
     case ADWIN_E_MODE:
-      return "unknown mode, reduction, dh_dtype, estimator or scheme, struct_bytes mismatch, or an "
-             "option the selected scheme does not offer";
+      return "unknown mode, reduction, dtype, estimator or scheme, struct_bytes mismatch, a temperature that is "
+             "not a positive normal number, or an option the selected scheme does not offer";
     case ADWIN_E_HIP: {
       const char* t = adwin::last_hip_error_text();
       return t[0] ? t : "a HIP call failed";
