@@ -595,6 +595,195 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
   }
 }
 
+// ---------------------------------------------------------------------------------------
+// The product, up to 256 tokens: one token tile of 64 FN, tiles of 128 entries, so that W is read once and the tiles spread evenly
+// over the compute units.  What bounds it is the read of W, and what counts is how much of it is under way: a ring of kStages
+// k-steps (128 bytes of 128 rows of W and of the tokens), all but one of them loading.  2 x 2 waves of 64 x 32 FN; operands,
+// fragments and their places in the LDS as in the kernel of many tokens.
+// ---------------------------------------------------------------------------------------
+template <int FN>
+struct MidTile {
+  static constexpr int kEntries = 128, kTokens = 64 * FN;
+  static constexpr int kBlockA = kEntries * 128, kStage = kBlockA + kTokens * 128;
+  static constexpr int kScratch = 4 * 4096;            // 32 tokens x 128 bytes of z for each wave
+  static constexpr int kStages = (160 * 1024 - kScratch) / kStage;
+  static constexpr int kLds = kStages * kStage + kScratch;
+  static constexpr int kLoads = 4 + 2 * FN;            // of a wave and stage
+};
+
+template <typename T, int FN>
+__global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
+  typedef MidTile<FN> Tile;
+  extern __shared__ __align__(16) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  const int block = xcd_contiguous_id(blockIdx.x, gridDim.x);
+  const int vt0 = (int)((int64_t)p.vocab_tiles * block / gridDim.x), vt1 = (int)((int64_t)p.vocab_tiles * (block + 1) / gridDim.x);
+  const int tiles = vt1 - vt0, nk = p.pitch / 128;
+  if (tiles <= 0) return;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+
+  const uint32_t chunk = (uint32_t)((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 16u;
+  const int e0 = 16 * half + 4 * wave + ((lane >> 3) & 3);
+  uint32_t voffa[4], voffb[2 * FN];
+  auto rows_of_w = [&](int tile) {                       // rows beyond V repeat the last one
+    const int64_t left = p.V - (int64_t)tile * Tile::kEntries - 1;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) voffa[d] = (uint32_t)(32 * d + e0 < left ? 32 * d + e0 : left) * (uint32_t)p.pitch + chunk;
+  };
+#pragma unroll
+  for (int d = 0; d < 2 * FN; ++d) {
+    const int64_t t = 32 * d + 8 * wave + (lane >> 3);
+    voffb[d] = (uint32_t)(t < p.T ? t : p.T - 1) * (uint32_t)p.pitch + chunk;
+  }
+  uint32_t swA[4], swB[4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) {
+    const uint32_t at = (lane & 31) * 128u + (uint32_t)(((2 * kk + half) ^ (lane >> 1)) & 7) * 16u;
+    swA[kk] = at + wa * (64 * 128);
+    swB[kk] = at + Tile::kBlockA + wb * (32 * FN * 128);
+  }
+  float sh[FN];
+#pragma unroll
+  for (int fn = 0; fn < FN; ++fn) {
+    const int64_t t = 32 * FN * wb + 32 * fn + (lane & 31);
+    sh[fn] = p.h_scale[t < p.T ? t : p.T - 1];
+    asm volatile("" : "+v"(sh[fn]));                     // waited for here
+  }
+
+  // where the next stage's loads come from: k-step kt of tile `tile` of the strip
+  int kt = 0, tile = 0;
+  const char* tile_w = (const char*)p.W + (int64_t)vt0 * Tile::kEntries * p.pitch;
+  uint32_t slot_w = lds0 + wave * 1024u;
+  rows_of_w(vt0);
+  auto ask = [&]() __attribute__((always_inline)) {
+    const char* a = tile_w + kt * 128;
+    const char* b = (const char*)p.h + kt * 128;
+#define Q_LOAD(D) dma16_at<(D) * 4096>(slot_w, voffa[D], a);
+    Q_LOAD(0) Q_LOAD(1) Q_LOAD(2) Q_LOAD(3)
+#undef Q_LOAD
+#define Q_LOAD(D) if constexpr ((D) < 2 * FN) dma16_at<Tile::kBlockA + (D) * 4096>(slot_w, voffb[(D) < 2 * FN ? (D) : 0], b);
+    Q_LOAD(0) Q_LOAD(1) Q_LOAD(2) Q_LOAD(3) Q_LOAD(4) Q_LOAD(5) Q_LOAD(6) Q_LOAD(7)
+#undef Q_LOAD
+    slot_w += Tile::kStage;
+    if (slot_w == lds0 + wave * 1024u + Tile::kStages * Tile::kStage) slot_w = lds0 + wave * 1024u;
+    if (++kt == nk) {                                    // behind the strip's last step its last tile again
+      kt = 0;
+      if (tile + 1 < tiles) {
+        ++tile;
+        tile_w += (int64_t)Tile::kEntries * p.pitch;
+        if ((int64_t)(vt0 + tile + 1) * Tile::kEntries > p.V) rows_of_w(vt0 + tile);
+      }
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < Tile::kStages - 1; ++s) ask();
+
+  // where the lane stores: token lane / 8 of 32, 16 bytes
+  constexpr int kPer = 16 / sizeof(T), kFms = sizeof(T) == 2 ? 2 : 1;     // blocks of 32 entries to 128 bytes
+  const uint32_t scratch = lds0 + Tile::kStages * Tile::kStage + wave * 4096u;
+  T* const z = (T*)p.z + (int64_t)(32 * FN * wb + (lane >> 3)) * p.ld_z + (lane & 7) * kPer;
+  const int rows_left = (int)(p.T - 32 * FN * wb - (lane >> 3));
+  uint32_t slot = lds0;
+  bool relaxed = false;
+  constexpr int kYounger = (Tile::kStages - 2) * Tile::kLoads, kStores = FN * (2 / kFms) * 4;
+  for (int i = 0; i < tiles; ++i) {
+    i32x16 acc[2][FN];
+#pragma unroll
+    for (int fm = 0; fm < 2; ++fm)
+#pragma unroll
+      for (int fn = 0; fn < FN; ++fn) acc[fm][fn] = i32x16{};
+    for (int k = 0; k < nk; ++k) {
+      // this step has landed (loads return in order; the stores of the tile before came behind its own), and every
+      // wave has read the step before, whose slot the next loads fill
+      if (k == 0 && relaxed) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kYounger + kStores < 63 ? kYounger + kStores : 63) : "memory");
+      else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kYounger) : "memory");
+      __syncthreads();
+      ask();
+      i32x4 fa[4][2], fb[4][FN];
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f) fa[kk][f] = q_frag(slot + swA[kk], 32 * f);
+#pragma unroll
+        for (int f = 0; f < FN; ++f) fb[kk][f] = q_frag(slot + swB[kk], 32 * f);
+      }
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int fm = 0; fm < 2; ++fm)
+#pragma unroll
+          for (int fn = 0; fn < FN; ++fn)
+            acc[fm][fn] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[kk][fm], fb[kk][fn], acc[fm][fn], 0, 0, 0);
+      slot += Tile::kStage;
+      if (slot == lds0 + Tile::kStages * Tile::kStage) slot = lds0;
+    }
+    const int64_t v0 = (int64_t)(vt0 + i) * Tile::kEntries + 64 * wa;
+    const int64_t left = p.V - v0;                       // may be 0 or less
+    relaxed = p.whole && left >= 64 && Tile::kTokens <= p.T;
+    if (left <= 0) continue;
+    float sv[2][16];
+    typedef const __attribute__((address_space(4))) float* Scales;
+#pragma unroll
+    for (int fm = 0; fm < 2; ++fm) {
+      if (left >= 64) {
+        uint64_t at = (uint64_t)(uintptr_t)(p.W_scale + v0 + 32 * fm);
+        asm volatile("" : "+s"(at));
+        const Scales s = (Scales)(uintptr_t)at;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float lo = s[e], hi = s[16 + e];
+          asm volatile("" : "+s"(lo), "+s"(hi));         // scalar loads: the loads in flight do not hold them up
+          sv[fm][e] = half ? hi : lo;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = 32 * fm + 16 * half + e;
+          sv[fm][e] = p.W_scale[v0 + (j < left ? j : left - 1)];
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(sv[fm][e]));
+      }
+    }
+    typedef __attribute__((address_space(3))) u32x4* LdsVec;
+#pragma unroll
+    for (int fn = 0; fn < FN; ++fn) {
+      if (32 * FN * wb + 32 * fn >= p.T) continue;
+#pragma unroll
+      for (int f0 = 0; f0 < 2; f0 += kFms) {
+#pragma unroll
+        for (int f = 0; f < kFms; ++f) {
+          float y[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] = (float)acc[f0 + f][fn][e] * (sh[fn] * sv[f0 + f][e]);
+#pragma unroll
+          for (int k = 0; k < 16 / kPer; ++k) {
+            const int at = (f * 32 + 16 * half) / kPer + k;
+            *(LdsVec)(uintptr_t)(scratch + (lane & 31) * 128u + (uint32_t)((at ^ (lane >> 1)) & 7) * 16u) = pack16(y + k * kPer, T{});
+          }
+        }
+        const int64_t n = left - 32 * f0 - (lane & 7) * kPer;      // of the lane's entries
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 8 * k + (lane >> 3);
+          const u32x4 row = *(LdsVec)(uintptr_t)(scratch + r * 128u + (uint32_t)(((lane & 7) ^ (r >> 1)) & 7) * 16u);
+          T* at = z + (int64_t)(32 * fn + 8 * k) * p.ld_z + v0 + 32 * f0;
+          if (rows_left > 32 * fn + 8 * k) {
+            if (p.whole && n >= kPer) *(u32x4*)at = row;
+            else {
+#pragma unroll
+              for (int e = 0; e < kPer; ++e)
+                if (e < n) at[e] = entry_of<T>(row, e);
+            }
+          }
+        }
+      }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads that nobody reads may still be writing the LDS
+}
+
 static int check_quant(const adwin_opd_quant_problem* p) {
   if (!p) return ADWIN_E_NULL;
   if (p->struct_bytes != sizeof(*p) || !known_dtype(p->x_dtype)) return ADWIN_E_MODE;
@@ -632,17 +821,26 @@ static int product_strips(int64_t tiles, int32_t vocab_tiles) {
   return strips;
 }
 
-// Groups of 16 tokens of the kernel for few tokens, 0 where the tiles serve the call: as many as fit the LDS, at most 4.
-static int few_tokens(int64_t T, int pitch) {
+// Groups of 16 tokens of the kernel for few tokens, 0 where others serve the call.  It takes as many as fit the LDS, at most 4; beyond
+// one group the tiles of 128 entries are as fast while there are two of them or fewer to a compute unit, and win there where the
+// tokens fill them.  us, few / tiles: 4 tokens, H = 1024, V = 32,000 14.8 / 14.5, 65,000 20.1 / 19.3, 100,000 25 / 29; 60 tokens
+// 17.0 / 15.8, 23.9 / 23.6, 29.5 / 34.4; H = 2048, V = 32,000 23.8 / 21.1, 65,000 37.4 / 34.0, 100,000 54 / 60; 48 tokens,
+// V = 151,936 77 / 83; 1 token, H = 4096 116 / 128, 32 tokens 131 / 139.
+static int few_tokens(int64_t T, int32_t V, int pitch) {
   const int64_t n = (T + 15) / 16;
-  return n <= 4 && few_lds((int)n, pitch) <= kQLds ? (int)n : 0;
+  return n <= 4 && (n == 1 || V > 2 * 128 * 256) && few_lds((int)n, pitch) <= kQLds ? (int)n : 0;
 }
+
+// Whether the kernel of one token tile and 128 entries serves the call.  Up to 128 tokens the read of W bounds it, and the smaller
+// tiles spread that over the compute units; beyond, the tiles of 256 entries do where they occupy more than half of
+// these.  us, 128 / 256 entries: V = 151,936, H = 4096: 33 tokens 139 / 171, 128 tokens 165 / 188, 192 tokens 214 / 196; 256 tokens,
+// H = 2048, V = 11,907 29 / 37, 32,000 33 / 39, 65,000 64 / 53, 100,000 103 / 89.
+static bool mid_tokens(int64_t T, int32_t V) { return T <= 128 || (T <= 256 && V <= 256 * 128); }
 
 template <typename T, int NT>
 static hipError_t launch_few_n(const ProductArgs& a, hipStream_t st) {
   const int groups = (a.V + 15) / 16;
-  int blocks = (groups + kFewWaves - 1) / kFewWaves;
-  if (blocks > 256) blocks = 256;
+  int blocks = groups < 256 ? groups : 256;
   if ((groups + blocks - 1) / blocks > kFewGroups) blocks = (groups + kFewGroups - 1) / kFewGroups;
   quant_few_kernel<T, NT><<<blocks, kFewThreads, few_lds(NT, a.pitch), st>>>(a);
   return hipGetLastError();
@@ -657,9 +855,23 @@ static hipError_t launch_few(const ProductArgs& a, int n, hipStream_t st) {
   }
 }
 
+template <typename T, int FN>
+static hipError_t launch_mid_n(const ProductArgs& a, hipStream_t st) {
+  quant_mid_kernel<T, FN><<<a.vocab_tiles < 256 ? a.vocab_tiles : 256, 256, MidTile<FN>::kLds, st>>>(a);
+  return hipGetLastError();
+}
+template <typename T>
+static hipError_t launch_mid(const ProductArgs& a, hipStream_t st) {
+  if (a.T <= 64) return launch_mid_n<T, 1>(a, st);
+  return a.T <= 128 ? launch_mid_n<T, 2>(a, st) : launch_mid_n<T, 4>(a, st);
+}
+
 // large dynamic LDS of the product, once per device
 hipError_t quant_kernels_opt_in() {
   for (const void* k : {(const void*)quant_tile_kernel<uint16_t>, (const void*)quant_tile_kernel<float>,
+                        (const void*)quant_mid_kernel<uint16_t, 1>, (const void*)quant_mid_kernel<uint16_t, 2>,
+                        (const void*)quant_mid_kernel<uint16_t, 4>, (const void*)quant_mid_kernel<float, 1>,
+                        (const void*)quant_mid_kernel<float, 2>, (const void*)quant_mid_kernel<float, 4>,
                         (const void*)quant_few_kernel<uint16_t, 1>, (const void*)quant_few_kernel<uint16_t, 2>,
                         (const void*)quant_few_kernel<uint16_t, 3>, (const void*)quant_few_kernel<uint16_t, 4>,
                         (const void*)quant_few_kernel<float, 1>, (const void*)quant_few_kernel<float, 2>,
@@ -729,9 +941,14 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
   const int64_t size = p->z_dtype == ADWIN_DT_BF16 ? 2 : 4;
   a.whole = ((uintptr_t)p->z & 15) == 0 && (p->ld_z * size & 15) == 0;
   ADWIN_HIP_TRY(quant_opt_in());
-  const int few = few_tokens(p->T, a.pitch);
+  const int few = few_tokens(p->T, p->V, a.pitch);
   if (few > 0) {
     ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_few<uint16_t>(a, few, stream) : launch_few<float>(a, few, stream));
+    return ADWIN_OK;
+  }
+  if (mid_tokens(p->T, p->V)) {
+    a.vocab_tiles = (p->V + 127) / 128;
+    ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_mid<uint16_t>(a, stream) : launch_mid<float>(a, stream));
     return ADWIN_OK;
   }
   const int64_t tiles = (p->T + kQTile - 1) / kQTile;
