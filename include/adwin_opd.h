@@ -409,7 +409,8 @@ int adwin_opd_from_logits_profile(const adwin_opd_logits_problem* p, void* works
  * alternatives, and the gradient of a loss on them.  The conventions above hold, except that
  * rows may lie any number of entries apart (`ld_*` >= the row's length) and that x, h, z and
  * dz need no more than the alignment of their entries; rows whose addresses are multiples of 16 bytes are
- * read and written 16 bytes at a time.  T (N) = 0 is a call that does nothing.
+ * read and written 16 bytes at a time.  (The order of a row's sums goes by where in 16 bytes it begins: the same logits
+ * there give the same bits.)  T (N) = 0 is a call that does nothing.
  *
  * Rows that cannot be computed are EXCLUDED, as in the calls above: zeros in every output (-1 in
  * top_ids), never an inf or NaN, and a bit of `row_status`, which is one word per row here.

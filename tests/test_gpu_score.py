@@ -47,7 +47,7 @@ def _quantised(x):
     fine = torch.isfinite(x.double()).all(dim=1, keepdim=True)
     a = torch.where(fine, a, 0.)
     q = torch.where(a > 0, torch.round(x.double() * 127 / torch.where(a > 0, a, 1)), 0.)
-    return q.to(torch.int8), (a.float() / 127)[:, 0], fine[:, 0]
+    return q.to(torch.int8), (a / 127).float()[:, 0], fine[:, 0]     # (on the GPU torch multiplies an fp32 tensor by 1 / 127)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -124,6 +124,25 @@ def test_quant_logits(B, T, V, H, h_dtype, z_dtype):
     assert torch.equal(view, got)
     flat[1:1 + T * (V + 3)].view(T, V + 3)[:, :V] = 7.0
     assert torch.all(flat == 7.0)
+
+
+@pytest.mark.parametrize("T,V,H", [(17, 70001, 128), (33, 70008, 250), (64, 66000, 256), (5, 600011, 128), (100, 70001, 384), (64, 90000, 2600),
+                                   (200, 40000, 128), (256, 33001, 384), (20, 131072, 4096)])
+def test_quant_logits_wide(B, T, V, H):
+    """Vocabularies of more tiles than there are compute units, where other kernels serve than above."""
+    g = torch.Generator("cuda").manual_seed(T)
+    h = torch.randn(T, H, generator=g, device="cuda").bfloat16()
+    W_q = torch.randint(-127, 128, (V, B.ADWIN_QUANT_PITCH(H)), generator=g, device="cuda", dtype=torch.int8)
+    W_q[:, H:] = 0
+    W_scale = torch.rand(V, generator=g, device="cuda") + 0.01
+    qh, sh, _ = _quantised(h)
+    for dtype in (torch.bfloat16, torch.float32):
+        got = B.adwin_opd_quant_logits(h, W_q, W_scale, z_dtype=B._DTYPE[dtype])["z"]
+        for lo in range(0, V, 16384):
+            W = W_q[lo:lo + 16384, :H].double()
+            want = (qh.double() @ W.t().contiguous()) * sh.double()[:, None] * W_scale[lo:lo + 16384].double()
+            tol = want.abs() * (3.01 * U + (torch.finfo(dtype).eps / 2 if dtype != torch.float32 else 0))
+            assert torch.all((got[:, lo:lo + 16384].double() - want).abs() <= tol), (dtype, lo)
 
 
 def test_quant_logits_largest_sums(B):
@@ -285,6 +304,35 @@ def test_token_logp_orders(B, dtype, T, V, order):
     ids = _ids(T, 2, V, 6)
     for top in (1, 13, 64):
         _check_logp(B, B.adwin_opd_token_logp(z.cuda(), ids.cuda(), top=top), z, ids, 1.0, top)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("order", ["rising", "falling", "equal", "two values", "late peak", "peak in one wave", "masked but few", "lowest but few",
+                                   "masked at first", "nan at last", "far at last"])
+def test_token_logp_many_long_rows(B, dtype, order):
+    """The same where a workgroup goes through a whole row in many steps: calls of many rows."""
+    T, V = 264, 30011
+    low = torch.finfo(dtype).min
+    z = torch.linspace(-8, 8, V).repeat(2, 1)
+    if order == "falling": z = z.flip(1)
+    if order == "equal": z = torch.full((2, V), 0.5)
+    if order == "two values": z = (torch.arange(V) % 3 == 0).float().repeat(2, 1)
+    if order in ("late peak", "nan at last", "far at last"): z = _logits(2, V, torch.float32, 3); z[:, V - V // 7:] += 12
+    if order == "peak in one wave": z = _logits(2, V, torch.float32, 5); z[:, (torch.arange(V) // 8) % 256 < 64] += 9
+    if order == "masked but few": z = torch.full((2, V), -math.inf); z[:, ::1000] = _logits(2, 31, torch.float32, 6)
+    if order == "lowest but few": z = torch.full((2, V), low); z[:, 5::1000] = _logits(2, 31, torch.float32, 6)[:, :len(range(5, V, 1000))]
+    if order == "masked at first": z = _logits(2, V, torch.float32, 7); z[:, :V - V // 8] = -math.inf
+    if order == "nan at last": z[1, V - 1] = math.nan
+    if order == "far at last": z[1, V - 2] = 1e30
+    z = z.to(dtype)
+    ids = torch.tensor([[3, 17], [V - 1, 5]], dtype=torch.int32)
+    many, many_ids = z.repeat(T // 2, 1).cuda(), ids.repeat(T // 2, 1).cuda()
+    for top in (1, 20, 64):
+        out = B.adwin_opd_token_logp(many, many_ids, top=top, row_status=True)
+        # sixteen rows begin at every place that 16 bytes have for a row; the order of its sums goes by that, and by nothing else
+        _check_logp(B, {k: v[:16] for k, v in out.items()}, z.repeat(8, 1), ids.repeat(8, 1), 1.0, top)
+        for k, v in out.items():
+            assert torch.equal(v[16:], v[:-16]), k
 
 
 def test_token_logp_small_forms(B):
