@@ -18,9 +18,13 @@ template <typename T>
 struct Eight {
   static constexpr int kVecs = (int)sizeof(T) / 2;
   u32x4 v[kVecs];
+  template <bool PAST>
   __device__ __forceinline__ void load(const T* x) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) v[i] = ((const u32x4*)x)[i];
+    for (int i = 0; i < kVecs; ++i) {
+      if constexpr (PAST) v[i] = __builtin_nontemporal_load((const u32x4*)x + i);
+      else v[i] = ((const u32x4*)x)[i];
+    }
   }
   // entries [0, n) of rows at any address, zeros behind them
   __device__ __forceinline__ void load_some(const T* x, int n) {
@@ -44,12 +48,21 @@ struct Eight {
   }
   // the larger of `top` and the magnitudes, as bits: a NaN counts as larger than inf
   __device__ __forceinline__ uint32_t largest(uint32_t top) const {
+    if constexpr (sizeof(T) == 2) {                    // two at a time, as 16-bit numbers
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      u16x2 m = __builtin_bit_cast(u16x2, v[0][0] & 0x7fff7fffu);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t b = __float_as_uint(entry(e)) & 0x7fffffffu;
-      top = b > top ? b : top;
+      for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[0][i] & 0x7fff7fffu));
+      const uint32_t b = (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16;
+      return b > top ? b : top;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t b = __float_as_uint(entry(e)) & 0x7fffffffu;
+        top = b > top ? b : top;
+      }
+      return top;
     }
-    return top;
   }
 };
 
@@ -63,10 +76,15 @@ __device__ __forceinline__ uint2 quantised(const Eight<T>& x, float per_a, float
   uint32_t b[8];
   float worst = tiny ? 1.f : 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float t = x.entry(e) * per_a, r = t + kWhole;
-    b[e] = __float_as_uint(r);
-    worst = fmaxf(worst, fabsf(t - (r - kWhole)));
+  for (int e = 0; e < 8; e += 2) {
+    float off[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float t = x.entry(e + i) * per_a, r = t + kWhole;
+      b[e + i] = __float_as_uint(r);
+      off[i] = t - (r - kWhole);
+    }
+    asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(worst) : "v"(off[0]), "v"(off[1]));
   }
   if (worst > 0.5f - 3.0e-5f) {
 #pragma unroll
@@ -82,18 +100,16 @@ __device__ __forceinline__ uint2 quantised(const Eight<T>& x, float per_a, float
 
 // One wave per row, eight entries to a lane and group.  Up to 4096 entries the row stays in registers between the search for
 // its largest magnitude and the integers; a longer one is read twice.  WHOLE: rows of whole groups that begin at multiples of
-// 16 bytes.  What bounds it is the memory.
+// 16 bytes.  What bounds it is the memory; PAST: past the caches, for arrays that they do not hold anyway.
 constexpr int kHeld = 8;                       // groups of a lane that are held
-template <typename T, bool WHOLE>
-__global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs p) {
+template <typename T, bool WHOLE, bool PAST>
+__device__ __forceinline__ void quant_row(const QuantArgs& p, int64_t n) {
   const int lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (n >= p.N) return;
   const T* x = (const T*)p.x + n * p.ld;
   const int groups = (p.H + 7) / 8;
   auto load = [&](Eight<T>& v, int g) __attribute__((always_inline)) {
     if constexpr (WHOLE) {
-      v.load(x + 8 * (g < groups ? g : groups - 1));   // straight-line loads: beyond the row its last group again
+      v.template load<PAST>(x + 8 * (g < groups ? g : groups - 1));   // straight-line loads: beyond the row its last group again
       if (g >= groups) v.clear();
     } else {
       v.load_some(x + 8 * g, p.H - 8 * g);
@@ -136,10 +152,19 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs p) {
       const int g = g0 + lane + 64 * i;
       if (g < out) {
         if (!held) load(v[i], g);
-        q[g] = a > 0.f ? quantised(v[i], per_a, a, tiny) : make_uint2(0, 0);
+        const uint2 o = a > 0.f ? quantised(v[i], per_a, a, tiny) : make_uint2(0, 0);
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        if constexpr (PAST) __builtin_nontemporal_store(u32x2{o.x, o.y}, (u32x2*)(q + g));
+        else q[g] = o;
       }
     }
   }
+}
+
+template <typename T, bool WHOLE, bool PAST>
+__global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs p) {
+  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (n < p.N) quant_row<T, WHOLE, PAST>(p, n);
 }
 
 struct ProductArgs {
@@ -884,16 +909,16 @@ hipError_t quant_kernels_opt_in() {
 static hipError_t quant_opt_in() { return first_use_on_device(2) ? quant_kernels_opt_in() : hipSuccess; }
 
 static hipError_t launch_quant_rows(const QuantArgs& a, int32_t dtype, hipStream_t st) {
-  const unsigned blocks = (unsigned)((a.N + 3) / 4);
+  const int64_t blocks = (a.N + 3) / 4;
   const int64_t size = dtype == ADWIN_DT_BF16 ? 2 : 4;
   const bool whole = ((uintptr_t)a.x & 15) == 0 && ((a.ld * size) & 15) == 0 && (a.H & 7) == 0;
-  if (dtype == ADWIN_DT_BF16) {
-    if (whole) quant_rows_kernel<uint16_t, true><<<blocks, 256, 0, st>>>(a);
-    else quant_rows_kernel<uint16_t, false><<<blocks, 256, 0, st>>>(a);
-  } else {
-    if (whole) quant_rows_kernel<float, true><<<blocks, 256, 0, st>>>(a);
-    else quant_rows_kernel<float, false><<<blocks, 256, 0, st>>>(a);
-  }
+  const bool past = whole && a.N * a.H * size > ((int64_t)320 << 20);
+#define ADWIN_LAUNCH(T)                                                                            \
+  if (past) quant_rows_kernel<T, true, true><<<(unsigned)blocks, 256, 0, st>>>(a);                 \
+  else if (whole) quant_rows_kernel<T, true, false><<<(unsigned)blocks, 256, 0, st>>>(a);          \
+  else quant_rows_kernel<T, false, false><<<(unsigned)blocks, 256, 0, st>>>(a);
+  if (dtype == ADWIN_DT_BF16) { ADWIN_LAUNCH(uint16_t) } else { ADWIN_LAUNCH(float) }
+#undef ADWIN_LAUNCH
   return hipGetLastError();
 }
 
