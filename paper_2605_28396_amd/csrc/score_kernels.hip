@@ -668,7 +668,9 @@ static int grad_pieces(int64_t T, int32_t V, int32_t dtype) {
 }
 
 // Whether an array of T x V is read (or written) past the caches: it is beyond the last-level cache of 256 MiB, so it has left
-// before anybody can find it there.
+// before anybody can find it there.  us, kept / past, bf16, V = 151,936: logp with 20 alternatives 600 rows 54.1 / 52.8 (kept, for the
+// gradient that reads the same logits), 1,300 rows 95 / 91, 8,192 rows 441 / 412; gradient 900 rows 115 / 116, 1,300 rows
+// 168 / 164, 2,000 rows 250 / 256, 8,192 rows 1006 / 962.
 static bool past_caches(int64_t T, int32_t V, int32_t dtype) {
   return T * V * (dtype == ADWIN_DT_BF16 ? 2 : 4) > ((int64_t)320 << 20);
 }
