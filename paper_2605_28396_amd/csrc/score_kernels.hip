@@ -78,28 +78,30 @@ __device__ __forceinline__ float add_entries(Sums& a, const float (&x)[N], float
   for (int i = 0; i < N; ++i) add_one(a, x[i], c);
   return m;
 }
-__device__ __forceinline__ void merge_sums(Sums& a, Sums b) {
-  if (b.r > a.r) { const Sums x = a; a = b; b = x; }
-  move_ref(b, a.r);
-  a.s += b.s;
-  a.t += b.t;
-  a.m = fmaxf(a.m, b.m);
+// Sums over the workgroup.  All move to the largest reference first, which multiplies them by powers of two.
+__device__ __forceinline__ Sums wave_sums(Sums a) {
+  move_ref(a, wave_max(a.r));
+  return {a.r, wave_sum(a.s), wave_sum(a.t), wave_max(a.m)};
 }
-
-__device__ __forceinline__ Sums block_sums(Sums a, float (*part)[4]) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const Sums b = {__shfl_xor(a.r, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.t, o, 64), __shfl_xor(a.m, o, 64)};
-    merge_sums(a, b);
-  }
+__device__ __forceinline__ Sums block_sums(const Sums& mine, float (*part)[4]) {
+  Sums a = wave_sums(mine);
   if ((threadIdx.x & 63) == 0) {
     float* q = part[threadIdx.x >> 6];
     q[0] = a.r; q[1] = a.s; q[2] = a.t; q[3] = a.m;
   }
   __syncthreads();
-  a = {part[0][0], part[0][1], part[0][2], part[0][3]};
+  float r = part[0][0];
+  a.m = part[0][3];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) merge_sums(a, Sums{part[w][0], part[w][1], part[w][2], part[w][3]});
+  for (int w = 1; w < kWaves; ++w) { r = fmaxf(r, part[w][0]); a.m = fmaxf(a.m, part[w][3]); }
+  a.r = r; a.s = 0.f; a.t = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    Sums b = {part[w][0], part[w][1], part[w][2], 0.f};
+    move_ref(b, r);
+    a.s += b.s;
+    a.t += b.t;
+  }
   return a;
 }
 
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       for (int u = 0; u < kStep; ++u) load_any(u);
 #pragma unroll
       for (int u = 0; u < kStep; ++u) {
-        if (__any(add(u) >= bound))
+        if (__any(i0 + kThreads * u < last) && __any(add(u) >= bound))
           list_entries<T>(l, listed, i0 + kThreads * u < last, v[u], p.row.index(i0 + tid + kThreads * u), bound);
       }
     }
