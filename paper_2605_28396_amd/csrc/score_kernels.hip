@@ -347,7 +347,10 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
   }
 }
 
-// One pass over the row, kStep vectors to a thread at a time.  What bounds it is the read of the logits.
+// One pass over the row, kStep vectors to a thread at a time.  8,192 rows (7,680 of them scored) of V = 151,936 bf16 with 20
+// alternatives: 377 to 390 us over boxes, 6.1 TB/s, without alternatives 365 us.  What bounds it is the read of the logits (a plain read of them 330 to 375 us) and, at
+// the clock of 2.1 GHz that it gets, the vector unit: 7.5 instructions an entry, 10 with what the alternatives take, busy
+// all the time; without the entropy's two of them it takes 377 us where it took 416.
 // The alternatives ride on the softmax's own maxima: the `top`-th largest of the threads' largest entries is a lower bound of the
 // `top`-th largest entry.  The first kStep vectors give one, what reaches it is listed (the bound is taken anew when twice as much
 // has been read), and at the end the threads' largest of all leave little more than `top` of these to rank.
@@ -573,7 +576,8 @@ struct GradRow {
   }
 };
 
-// A workgroup per piece of a row.  What bounds it is the read of z and the write of dz, PAST the caches where they exceed them.
+// A workgroup per piece of a row.  What bounds it is the read of z and the write of dz, PAST the caches where they exceed them:
+// 8,192 rows (7,168 of them scored) of V = 151,936 bf16 915 us, 5.1 TB/s; 777 x 32,771 fp32 34 us, 5.6 TB/s.  kStep of 2 or 8: 932, 918 us.
 template <typename TI, typename TO, bool PAST>
 __global__ __launch_bounds__(kThreads) void token_logp_grad_kernel(LogpGradArgs a) {
   constexpr int N = Entry<TI>::kPerVec;
