@@ -630,8 +630,9 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
 }
 
 // ---------------------------------------------------------------------------------------
-// The product, up to 256 tokens: one token tile of 64 FN, tiles of 128 entries, so that W is read once and the tiles spread evenly
-// over the compute units.  What bounds it is the read of W, and what counts is how much of it is under way: a ring of kStages
+// The product in smaller tiles, 64 FN tokens x 128 entries: for one token tile, so that W is read once and its tiles spread evenly
+// over the compute units, and for products that large tiles would not spread over them at all.  What bounds it is the read of W, or
+// latency, and what counts is how much is under way: a ring of kStages
 // k-steps (128 bytes of 128 rows of W and of the tokens), all but one of them loading.  2 x 2 waves of 64 x 32 FN; operands,
 // fragments and their places in the LDS as in the kernel of many tokens.  V = 151,936, H = 4096: 64 tokens 145 us with the rows'
 // integers (4.4 TB/s), 128 tokens 165 us; 1,187 tiles are 4.6 rounds of 256 compute units and run as 5.
@@ -652,8 +653,11 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
   extern __shared__ __align__(16) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave & 1, wb = wave >> 1, half = lane >> 5;
-  const int block = xcd_contiguous_id(blockIdx.x, gridDim.x);
-  const int vt0 = (int)((int64_t)p.vocab_tiles * block / gridDim.x), vt1 = (int)((int64_t)p.vocab_tiles * (block + 1) / gridDim.x);
+  int strip, tt;
+  strip_and_tile(xcd_contiguous_id(blockIdx.x, gridDim.x), p.group, p.strips, p.token_tiles, &strip, &tt);
+  const int vt0 = (int)((int64_t)p.vocab_tiles * strip / p.strips), vt1 = (int)((int64_t)p.vocab_tiles * (strip + 1) / p.strips);
+  const int64_t t0 = (int64_t)tt * Tile::kTokens, T_left = p.T - t0;       // tokens from this tile on
+  const char* const h = (const char*)p.h + t0 * p.pitch;
   const int tiles = vt1 - vt0, nk = p.pitch / 128;
   if (tiles <= 0) return;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
@@ -669,7 +673,7 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
 #pragma unroll
   for (int d = 0; d < 2 * FN; ++d) {
     const int64_t t = 32 * d + 8 * wave + (lane >> 3);
-    voffb[d] = (uint32_t)(t < p.T ? t : p.T - 1) * (uint32_t)p.pitch + chunk;
+    voffb[d] = (uint32_t)(t < T_left ? t : T_left - 1) * (uint32_t)p.pitch + chunk;
   }
   uint32_t swA[4], swB[4];
 #pragma unroll
@@ -682,7 +686,7 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
 #pragma unroll
   for (int fn = 0; fn < FN; ++fn) {
     const int64_t t = 32 * FN * wb + 32 * fn + (lane & 31);
-    sh[fn] = p.h_scale[t < p.T ? t : p.T - 1];
+    sh[fn] = p.h_scale[t0 + (t < T_left ? t : T_left - 1)];
     asm volatile("" : "+v"(sh[fn]));                     // waited for here
   }
 
@@ -693,7 +697,7 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
   rows_of_w(vt0);
   auto ask = [&]() __attribute__((always_inline)) {
     const char* a = tile_w + kt * 128;
-    const char* b = (const char*)p.h + kt * 128;
+    const char* b = h + kt * 128;
 #define Q_LOAD(D) dma16_at<(D) * 4096>(slot_w, voffa[D], a);
     Q_LOAD(0) Q_LOAD(1) Q_LOAD(2) Q_LOAD(3)
 #undef Q_LOAD
@@ -717,8 +721,8 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
   // where the lane stores: token lane / 8 of 32, 16 bytes
   constexpr int kPer = 16 / sizeof(T), kFms = sizeof(T) == 2 ? 2 : 1;     // blocks of 32 entries to 128 bytes
   const uint32_t scratch = lds0 + Tile::kStages * Tile::kStage + wave * 4096u;
-  T* const z = (T*)p.z + (int64_t)(32 * FN * wb + (lane >> 3)) * p.ld_z + (lane & 7) * kPer;
-  const int rows_left = (int)(p.T - 32 * FN * wb - (lane >> 3));
+  T* const z = (T*)p.z + (t0 + 32 * FN * wb + (lane >> 3)) * p.ld_z + (lane & 7) * kPer;
+  const int rows_left = (int)(T_left < Tile::kTokens ? T_left : Tile::kTokens) - 32 * FN * wb - (lane >> 3);
   uint32_t slot = lds0;
   bool relaxed = false;
   constexpr int kYounger = (Tile::kStages - 2) * Tile::kLoads, kStores = FN * (2 / kFms) * 4;
@@ -755,7 +759,7 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
     }
     const int64_t v0 = (int64_t)(vt0 + i) * Tile::kEntries + 64 * wa;
     const int64_t left = p.V - v0;                       // may be 0 or less
-    relaxed = p.whole && left >= 64 && Tile::kTokens <= p.T;
+    relaxed = p.whole && left >= 64 && Tile::kTokens <= T_left;
     if (left <= 0) continue;
     float sv[2][16];
     typedef const __attribute__((address_space(4))) float* Scales;
@@ -784,7 +788,7 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
     typedef __attribute__((address_space(3))) u32x4* LdsVec;
 #pragma unroll
     for (int fn = 0; fn < FN; ++fn) {
-      if (32 * FN * wb + 32 * fn >= p.T) continue;
+      if (32 * FN * wb + 32 * fn >= T_left) continue;
 #pragma unroll
       for (int f0 = 0; f0 < 2; f0 += kFms) {
 #pragma unroll
@@ -845,32 +849,49 @@ struct QuantLayout {
 };
 
 // Strips of the vocabulary for `tiles` token tiles: one workgroup occupies a compute unit, so that what counts is the number of
-// rounds times the tiles of the longest strip.
-static int product_strips(int64_t tiles, int32_t vocab_tiles) {
+// rounds times the tiles of the longest strip (*turns); of as good ones in a single round the most.
+static int product_strips(int64_t tiles, int32_t vocab_tiles, int64_t* turns = nullptr) {
   int64_t best = 0;
   int strips = 1;
   for (int s = 1; s <= vocab_tiles && s <= 256; ++s) {
     const int64_t cost = (tiles * s + 255) / 256 * ((vocab_tiles + s - 1) / s);
-    if (best == 0 || cost < best) { best = cost; strips = s; }
+    if (best == 0 || cost < best || (cost == best && tiles * s <= 256)) { best = cost; strips = s; }
   }
+  if (turns) *turns = best;
   return strips;
 }
 
-// Groups of 16 tokens of the kernel for few tokens, 0 where others serve the call.  It takes as many as fit the LDS, at most 4; beyond
-// one group the tiles of 128 entries are as fast while there are two of them or fewer to a compute unit, and win there where the
-// tokens fill them.  us, few / tiles: 4 tokens, H = 1024, V = 32,000 14.8 / 14.5, 65,000 20.1 / 19.3, 100,000 25 / 29; 60 tokens
-// 17.0 / 15.8, 23.9 / 23.6, 29.5 / 34.4; H = 2048, V = 32,000 23.8 / 21.1, 65,000 37.4 / 34.0, 100,000 54 / 60; 48 tokens,
-// V = 151,936 77 / 83; 1 token, H = 4096 116 / 128, 32 tokens 131 / 139.
-static int few_tokens(int64_t T, int32_t V, int pitch) {
-  const int64_t n = (T + 15) / 16;
-  return n <= 4 && (n == 1 || V > 2 * 128 * 256) && few_lds((int)n, pitch) <= kQLds ? (int)n : 0;
+// The tile of a product: 64 or 128 tokens x 128 entries (1, 2), or 256 x 256 (0).  What a call takes is near
+// first + turns (tile + k-steps step), turns being the tiles that the busiest compute unit goes through one after the other; the
+// numbers (us) are fitted to the calls below, whose times they give to 15 % and whose order they keep.  us, 256 x 256 / 128 x 128 / 64 x 128
+// (with 5 for the tokens' integers): 1,000 tokens, V = 2,000, H = 1024 25.8 / 14.3 / 12.0, H = 4096 54 / 30 / 25; V = 8,000,
+// H = 2048 38 / 31 / 37; 701 tokens, V = 11,907, H = 632 24.2 / 22.2 / 24.5; 400 tokens, V = 32,000, H = 1024 27.5 / 31.5 / 37.4; 600 tokens,
+// V = 50,000 63 / 58 / 76; 2,048 tokens, V = 16,000, H = 2048 77 / 94 / 118; 300 tokens, V = 151,936, H = 1024 98 / 93 / 115, 100 tokens, H = 4096
+// 186 / 155, 192 tokens 196.
+static int product_tile(int64_t T, int32_t V, int pitch) {
+  struct Way { int tokens, entries; double first, tile, step; };
+  constexpr Way ways[3] = {{256, 256, 5.0, 6.0, 1.25}, {64, 128, 2.2, 0.5, 0.45}, {128, 128, 2.5, 1.5, 0.62}};
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < 3; ++i) {
+    int64_t turns;
+    product_strips((T + ways[i].tokens - 1) / ways[i].tokens, (V + ways[i].entries - 1) / ways[i].entries, &turns);
+    const double us = ways[i].first + (double)turns * (ways[i].tile + pitch / 128 * ways[i].step);
+    if (i == 0 || us < least) { least = us; best = i; }
+  }
+  return best;
 }
 
-// Whether the kernel of one token tile and 128 entries serves the call.  Up to 128 tokens the read of W bounds it, and the smaller
-// tiles spread that over the compute units; beyond, the tiles of 256 entries do where they occupy more than half of
-// these.  us, 128 / 256 entries: V = 151,936, H = 4096: 33 tokens 139 / 171, 128 tokens 165 / 188, 192 tokens 214 / 196; 256 tokens,
-// H = 2048, V = 11,907 29 / 37, 32,000 33 / 39, 65,000 64 / 53, 100,000 103 / 89.
-static bool mid_tokens(int64_t T, int32_t V) { return T <= 128 || (T <= 256 && V <= 256 * 128); }
+// Groups of 16 tokens of the kernel for few tokens, 0 where tiles serve the call: as many as fit the LDS, at most 4, but for more than
+// two where one or two tiles of 128 entries to a compute unit spread as well and are filled by the tokens.  us, few / tiles: 1 token,
+// H = 1024, V = 1,000 7.5 / 10.2, V = 151,936 30.5 / 33.2, H = 4096, V = 4,000 11.5 / 19.3; 16 tokens, H = 4096, V = 16,000 21.4 / 21.1,
+// H = 2048, V = 50,000 24.8 / 25.8; 30 tokens, H = 4096, V = 40,000 35.6 / 41.2; 40 tokens, H = 1024, V = 4,000 9.1 / 10.9,
+// H = 2048, V = 16,000 14.3 / 14.7; 60 tokens, V = 30,000 22.1 / 18.1, V = 75,000 35.2 / 36.8, H = 1024, V = 60,000 21.5 / 19.7.
+static int few_tokens(int64_t T, int32_t V, int pitch) {
+  const int64_t n = (T + 15) / 16;
+  const bool suits = n <= 2 || V <= 128 * 128 || V > 2 * 128 * 256;
+  return n <= 4 && suits && few_lds((int)n, pitch) <= kQLds ? (int)n : 0;
+}
 
 template <typename T, int NT>
 static hipError_t launch_few_n(const ProductArgs& a, hipStream_t st) {
@@ -891,22 +912,20 @@ static hipError_t launch_few(const ProductArgs& a, int n, hipStream_t st) {
 }
 
 template <typename T, int FN>
-static hipError_t launch_mid_n(const ProductArgs& a, hipStream_t st) {
-  quant_mid_kernel<T, FN><<<a.vocab_tiles < 256 ? a.vocab_tiles : 256, 256, MidTile<FN>::kLds, st>>>(a);
+static hipError_t launch_mid(const ProductArgs& a, hipStream_t st) {
+  ProductArgs b = a;
+  b.token_tiles = (int32_t)((a.T + MidTile<FN>::kTokens - 1) / MidTile<FN>::kTokens);
+  b.vocab_tiles = (a.V + 127) / 128;
+  b.strips = product_strips(b.token_tiles, b.vocab_tiles);
+  b.group = 4;
+  quant_mid_kernel<T, FN><<<(unsigned)(b.token_tiles * b.strips), 256, MidTile<FN>::kLds, st>>>(b);
   return hipGetLastError();
 }
-template <typename T>
-static hipError_t launch_mid(const ProductArgs& a, hipStream_t st) {
-  if (a.T <= 64) return launch_mid_n<T, 1>(a, st);
-  return a.T <= 128 ? launch_mid_n<T, 2>(a, st) : launch_mid_n<T, 4>(a, st);
-}
-
 // large dynamic LDS of the product, once per device
 hipError_t quant_kernels_opt_in() {
   for (const void* k : {(const void*)quant_tile_kernel<uint16_t>, (const void*)quant_tile_kernel<float>,
                         (const void*)quant_mid_kernel<uint16_t, 1>, (const void*)quant_mid_kernel<uint16_t, 2>,
-                        (const void*)quant_mid_kernel<uint16_t, 4>, (const void*)quant_mid_kernel<float, 1>,
-                        (const void*)quant_mid_kernel<float, 2>, (const void*)quant_mid_kernel<float, 4>,
+                        (const void*)quant_mid_kernel<float, 1>, (const void*)quant_mid_kernel<float, 2>,
                         (const void*)quant_few_kernel<uint16_t, 1>, (const void*)quant_few_kernel<uint16_t, 2>,
                         (const void*)quant_few_kernel<uint16_t, 3>, (const void*)quant_few_kernel<uint16_t, 4>,
                         (const void*)quant_few_kernel<float, 1>, (const void*)quant_few_kernel<float, 2>,
@@ -983,9 +1002,10 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
     ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_few<uint16_t>(a, few, stream) : launch_few<float>(a, few, stream));
     return ADWIN_OK;
   }
-  if (mid_tokens(p->T, p->V)) {
-    a.vocab_tiles = (p->V + 127) / 128;
-    ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_mid<uint16_t>(a, stream) : launch_mid<float>(a, stream));
+  if (const int way = product_tile(p->T, p->V, a.pitch)) {
+    const bool bf16 = p->z_dtype == ADWIN_DT_BF16;
+    ADWIN_HIP_TRY(way == 1 ? (bf16 ? launch_mid<uint16_t, 1>(a, stream) : launch_mid<float, 1>(a, stream))
+                           : (bf16 ? launch_mid<uint16_t, 2>(a, stream) : launch_mid<float, 2>(a, stream)));
     return ADWIN_OK;
   }
   const int64_t tiles = (p->T + kQTile - 1) / kQTile;
