@@ -127,7 +127,8 @@ def test_quant_logits(B, T, V, H, h_dtype, z_dtype):
 
 
 @pytest.mark.parametrize("T,V,H", [(17, 70001, 128), (33, 70008, 250), (64, 66000, 256), (5, 600011, 128), (100, 70001, 384), (64, 90000, 2600),
-                                   (200, 40000, 128), (256, 33001, 384), (20, 131072, 4096)])
+                                   (200, 40000, 128), (256, 33001, 384), (20, 131072, 4096), (400, 32003, 1000), (777, 33001, 1500), (300, 30000, 2000), (256, 50001, 4000),
+                                   (140, 70001, 4096), (500, 60007, 700), (3000, 40010, 250), (2050, 66003, 256), (4000, 33000, 384)])
 def test_quant_logits_wide(B, T, V, H):
     """Vocabularies of more tiles than there are compute units, where other kernels serve than above."""
     g = torch.Generator("cuda").manual_seed(T)
@@ -143,6 +144,21 @@ def test_quant_logits_wide(B, T, V, H):
             want = (qh.double() @ W.t().contiguous()) * sh.double()[:, None] * W_scale[lo:lo + 16384].double()
             tol = want.abs() * (3.01 * U + (torch.finfo(dtype).eps / 2 if dtype != torch.float32 else 0))
             assert torch.all((got[:, lo:lo + 16384].double() - want).abs() <= tol), (dtype, lo)
+
+
+def test_quant_logits_of_one_k_step(B):
+    """Tiles whose whole contraction is one k-step: the loads run two tiles ahead."""
+    T, V, H = 8200, 150001, 100
+    g = torch.Generator("cuda").manual_seed(3)
+    h = torch.randn(T, H, generator=g, device="cuda")
+    W_q = torch.randint(-127, 128, (V, 128), generator=g, device="cuda", dtype=torch.int8)
+    W_q[:, H:] = 0
+    W_scale = torch.rand(V, generator=g, device="cuda") + 0.01
+    qh, sh, _ = _quantised(h)
+    got = B.adwin_opd_quant_logits(h, W_q, W_scale)["z"]
+    for lo in range(0, V, 8192):
+        want = (qh.double() @ W_q[lo:lo + 8192, :H].double().t().contiguous()) * sh.double()[:, None] * W_scale[lo:lo + 8192].double()
+        assert torch.all((got[:, lo:lo + 8192].double() - want).abs() <= want.abs() * (3.01 * U + 2.0 ** -8)), lo
 
 
 def test_quant_logits_largest_sums(B):
