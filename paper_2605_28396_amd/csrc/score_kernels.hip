@@ -127,6 +127,7 @@ struct Select {                    // in the LDS
   uint64_t dense[kDense];
   uint64_t best[kThreads + 1];
   uint32_t most[kThreads];         // the threads' largest entries, as order_bits >> 16
+  uint32_t bounds[kWaves];         // of the waves' maxima (lanes_bound)
   int listed[kWaves];
   int count;
 };
@@ -149,6 +150,25 @@ __device__ __forceinline__ uint32_t wave_bound(const volatile uint32_t* most, in
   }
   return at;
 }
+// The same of a wave's 64 numbers: a quarter of the work.  Where each of the four waves has top / 4 threads whose largest entry reaches a
+// number, `top` entries do: the least of the waves' numbers is a bound as well, and little below the exact one unless the
+// waves, which take 512 entries in turn, see different rows.
+__device__ __forceinline__ uint32_t lanes_bound(uint32_t mine, int n) {
+  uint32_t at = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t t = at | (1u << bit);
+    if (__popcll(__ballot(mine >= t)) >= n) at = t;
+  }
+  return at;
+}
+__device__ __forceinline__ uint32_t least_bound(const volatile uint32_t* bounds) {
+  uint32_t at = bounds[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) { const uint32_t b = bounds[w]; at = b < at ? b : at; }
+  return at;
+}
+
 // the smallest logit whose order_bits reach at << 16
 __device__ __forceinline__ float bound_value(uint32_t at) {
   if (at <= 0x007fu) return -INFINITY;              // order_bits(-inf) = 0x007fffff
@@ -160,8 +180,12 @@ __device__ __forceinline__ float bound_value(uint32_t at) {
 __device__ __forceinline__ void rank_keys(Select& l, const uint64_t* keys, int n, int top) {
   for (int q = threadIdx.x; q < n; q += kThreads) {
     const uint64_t v = keys[q];
-    int r = 0;
-    for (int j = 0; j < n; ++j) r += keys[j] > v;
+    int r = 0, j = 0;
+    for (; j + 8 <= n; j += 8) {                   // eight reads of the LDS at a time
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r += keys[j + i] > v;
+    }
+    for (; j < n; ++j) r += keys[j] > v;
     if (r < top) l.kept[r] = v;
   }
   if ((int)threadIdx.x >= n && (int)threadIdx.x < top) l.kept[threadIdx.x] = 0;
@@ -220,8 +244,9 @@ __device__ __forceinline__ void select_slowly(const Piece<T>& p, int top, Select
 }
 
 // What the waves have listed (`listed` keys of this one) and reaches the bound of the threads' largest entries, ranked.  Every
-// thread has written its `most`.  False where more was found than could be listed or can be ranked.
-__device__ __forceinline__ bool select_found(Select& l, int listed, int top) {
+// wave has written its bound; `again`: since the one was taken that the listed keys reach.  False where more was found
+// than could be listed or can be ranked.
+__device__ __forceinline__ bool select_found(Select& l, int listed, int top, bool again) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (lane == 0) l.listed[wave] = listed;
   if (threadIdx.x == 0) l.count = 0;
@@ -230,7 +255,7 @@ __device__ __forceinline__ bool select_found(Select& l, int listed, int top) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) fits = fits && l.listed[w] <= kPart;
   if (!fits) return false;
-  const uint64_t bound = (uint64_t)wave_bound(l.most, top) << 48;
+  const uint64_t bound = again ? (uint64_t)least_bound(l.bounds) << 48 : 0;
   uint64_t key[kPart / 64];
   int n = 0;
 #pragma unroll
@@ -360,7 +385,6 @@ template <typename T, bool PAST>
 __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
   constexpr int N = Entry<T>::kPerVec;
   __shared__ Select l;
-  __shared__ float shared_bound;
   __shared__ float part[kWaves][4];
   const int tid = threadIdx.x;
   const int64_t r = blockIdx.x / (uint32_t)a.pieces;
@@ -403,11 +427,15 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
     // the first vectors, which give the first bound and are then gone through again
 #pragma unroll
     for (int u = 0; u < kStep; ++u) add(u);
+    const int quarter = (a.top + kWaves - 1) / kWaves;
+    auto take_bound = [&]() {                       // a thread without entries: -inf
+      const uint32_t at = lanes_bound(order_bits(sum.m) >> 16, quarter);
+      if ((tid & 63) == 0) *(volatile uint32_t*)&l.bounds[tid >> 6] = at;
+    };
     if (a.top > 0) {
-      l.most[tid] = order_bits(sum.m) >> 16;        // a thread without entries: -inf
+      take_bound();
       __syncthreads();
-      bound = bound_value(wave_bound(l.most, a.top));
-      if (tid == 0) shared_bound = bound;
+      bound = bound_value(least_bound(l.bounds));
       list_entry(l, listed, tid < p.edge && edge[0] >= bound, edge[0], p.row.edge_index(tid));
 #pragma unroll
       for (int u = 0; u < kStep; ++u)
@@ -419,17 +447,10 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       for (int u = 0; u < kStep; ++u) load(u);
     }
     for (int step = 1; step < whole; ++step) {
-      if (a.top > 0) {
-        // A new bound at steps 1, 2, 4, 8, ..., by one wave in turn.  An older maximum of a thread gives a bound as well,
-        // and so does an older bound: nobody waits.
-        if ((step & (step - 1)) == 0) {
-          *(volatile uint32_t*)&l.most[tid] = order_bits(sum.m) >> 16;
-          if ((tid >> 6) == (__ffs(step) & (kWaves - 1))) {
-            const float b = bound_value(wave_bound(l.most, a.top));
-            if ((tid & 63) == 0) *(volatile float*)&shared_bound = b;
-          }
-        }
-        bound = fmaxf(bound, *(volatile float*)&shared_bound);
+      if (a.top > 0 && (step & (step - 1)) == 0) {
+        // A new bound at steps 1, 2, 4, 8, ....  An older one of another wave is a bound as well: nobody waits.
+        take_bound();
+        bound = fmaxf(bound, bound_value(least_bound(l.bounds)));
       }
       const int first = p.row.index(i0 + tid);
       i0 += kStep * kThreads;
@@ -455,9 +476,8 @@ __global__ __launch_bounds__(kThreads, 6) void token_logp_kernel(LogpArgs a) {
       }
     }
     if (a.top > 0) {
-      __syncthreads();                              // all have read the first bound
-      l.most[tid] = order_bits(sum.m) >> 16;
-      if (!select_found(l, listed, a.top)) select_slowly(p, a.top, l);
+      if (whole > 0) take_bound();
+      if (!select_found(l, listed, a.top, whole > 0)) select_slowly(p, a.top, l);
     }
     sum = piece_sums(p, sum, a.c, part);
   }
