@@ -430,7 +430,7 @@ int adwin_opd_from_logits_profile(const adwin_opd_logits_problem* p, void* works
 /* Rows to 8-bit integers with one scale per row: with a = max_j |x_j|,
  *   scale = a / 127,   q_j = 127 x_j / a to the nearest integer, ties to the even one,
  * so that x_j is scale q_j to half a step.  A row of zeros has scale 0.  A row with an inf or NaN is excluded:
- * scale 0, q 0, ADWIN_DEV_NONFINITE in row_status.  Limits: 0 <= N < 2^31, 1 <= H <= ADWIN_QUANT_MAX_H. */
+ * scale 0, q 0, ADWIN_DEV_NONFINITE in row_status.  Limits: 0 <= N < 2^24, 1 <= H <= ADWIN_QUANT_MAX_H. */
 typedef struct adwin_opd_quant_problem {
   size_t  struct_bytes;      /* sizeof(adwin_opd_quant_problem), checked                       */
   int64_t N;                 /* rows                                                           */
@@ -448,7 +448,7 @@ int adwin_opd_quant_rows(const adwin_opd_quant_problem* p, void* hip_stream);
  *   z[t, v] = s_h[t] W_scale[v] sum_k q_h[t, k] W_q[v, k],
  * the sum exact in 32-bit integers, one rounding of it to fp32 and one of z to its type.  The head is
  * adwin_opd_quant_rows of W [V, H]: laid out once, or whenever the weights change.
- * Limits: 0 <= T < 2^31, 1 <= V <= 2^28, 1 <= H <= ADWIN_QUANT_MAX_H. */
+ * Limits: 0 <= T < 2^24, 1 <= V <= 2^28, 1 <= H <= ADWIN_QUANT_MAX_H. */
 typedef struct adwin_opd_quant_logits_problem {
   size_t  struct_bytes;
   int64_t T;
@@ -475,7 +475,7 @@ int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, void* worksp
  * ADWIN_DEV_BAD_ID.  A row of which no id is scored is not computed: zeros, -1 in top_ids (rows outside a
  * window are given so).  With G = 0 every row is computed.  A row with a NaN or +inf, or of nothing but -inf,
  * is excluded with ADWIN_DEV_NONFINITE.
- * Limits: 0 <= T < 2^31, 1 <= V <= 2^28, 0 <= G <= ADWIN_MAX_GIVEN, 0 <= top <= ADWIN_MAX_TOP. */
+ * Limits: 0 <= T < 2^24, 1 <= V <= 2^28, 0 <= G <= ADWIN_MAX_GIVEN, 0 <= top <= ADWIN_MAX_TOP. */
 typedef struct adwin_opd_logp_problem {
   size_t  struct_bytes;
   int64_t T;

@@ -1013,7 +1013,6 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
   a.vocab_tiles = (p->V + kQTile - 1) / kQTile;
   a.strips = product_strips(tiles, a.vocab_tiles);
   a.group = 4;
-  if (tiles * a.strips >= kMaxRows) return ADWIN_E_SHAPE;
   const unsigned blocks = (unsigned)(tiles * a.strips);
   if (p->z_dtype == ADWIN_DT_BF16) quant_tile_kernel<uint16_t><<<blocks, 256, kQLds, stream>>>(a);
   else quant_tile_kernel<float><<<blocks, 256, kQLds, stream>>>(a);

@@ -89,7 +89,7 @@ struct RowSpan {
 
 inline bool known_dtype(int32_t d) { return d == ADWIN_DT_BF16 || d == ADWIN_DT_F32; }
 inline uintptr_t entry_mask(int32_t d) { return d == ADWIN_DT_BF16 ? 1 : 3; }
-constexpr int64_t kMaxRows = (int64_t)1 << 31;      // rows of a call: fewer than this
+constexpr int64_t kMaxRows = (int64_t)1 << 24;      // rows of a call: fewer than this (a launch has fewer than 2^32 threads)
 constexpr int32_t kMaxVocab = 1 << 28;
 
 }  // namespace adwin

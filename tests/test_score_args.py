@@ -50,7 +50,7 @@ def test_quant_rows_refusals(B):
         return B.lib.adwin_opd_quant_rows(C.byref(_struct(B.adwin_opd_quant_problem, base, over)), None)
     assert B.lib.adwin_opd_quant_rows(None, None) == B.ADWIN_E_NULL
     assert st(struct_bytes=8) == B.ADWIN_E_MODE and st(x_dtype=2) == B.ADWIN_E_MODE
-    for over in (dict(H=0), dict(H=B.ADWIN_QUANT_MAX_H + 1, ld_x=1 << 20), dict(N=-1), dict(N=1 << 31), dict(ld_x=63)):
+    for over in (dict(H=0), dict(H=B.ADWIN_QUANT_MAX_H + 1, ld_x=1 << 20), dict(N=-1), dict(N=1 << 24), dict(N=1 << 31), dict(ld_x=63)):
         assert st(**over) == B.ADWIN_E_SHAPE, over
     for over in (dict(x=None), dict(q=None), dict(scale=None)):
         assert st(**over) == B.ADWIN_E_NULL, over
@@ -72,7 +72,7 @@ def test_quant_logits_refusals(B):
     assert B.lib.adwin_opd_quant_logits(None, PTR, need, None) == B.ADWIN_E_NULL
     assert B.lib.adwin_opd_quant_logits_workspace_bytes(C.byref(p()), None) == B.ADWIN_E_NULL
     assert st(struct_bytes=8) == st(h_dtype=5) == st(z_dtype=-1) == B.ADWIN_E_MODE
-    for over in (dict(H=0), dict(V=0), dict(V=(1 << 28) + 1, ld_z=1 << 29), dict(T=-1), dict(T=1 << 31), dict(ld_h=63),
+    for over in (dict(H=0), dict(V=0), dict(V=(1 << 28) + 1, ld_z=1 << 29), dict(T=-1), dict(T=1 << 24), dict(T=1 << 31), dict(ld_h=63),
                  dict(ld_z=999), dict(H=B.ADWIN_QUANT_MAX_H + 1, ld_h=1 << 20)):
         assert st(**over) == B.ADWIN_E_SHAPE, over
     for name in ("h", "W_q", "W_scale", "z"):
@@ -95,7 +95,7 @@ def test_token_logp_refusals(B):
     assert st(struct_bytes=8) == st(z_dtype=2) == B.ADWIN_E_MODE
     for t in (0.0, -1.0, float("nan"), float("inf"), 1e-40):
         assert st(temperature=t) == B.ADWIN_E_MODE, t
-    for over in (dict(V=0), dict(V=(1 << 28) + 1, ld_z=1 << 29), dict(T=-1), dict(T=1 << 31), dict(ld_z=999), dict(G=-1),
+    for over in (dict(V=0), dict(V=(1 << 28) + 1, ld_z=1 << 29), dict(T=-1), dict(T=1 << 24), dict(T=1 << 31), dict(ld_z=999), dict(G=-1),
                  dict(G=B.ADWIN_MAX_GIVEN + 1), dict(top=-1), dict(top=B.ADWIN_MAX_TOP + 1)):
         assert st(**over) == B.ADWIN_E_SHAPE, over
     assert st(z=None) == st(ids=None) == B.ADWIN_E_NULL
@@ -115,7 +115,7 @@ def test_token_logp_grad_refusals(B):
         return B.lib.adwin_opd_token_logp_grad(C.byref(_struct(B.adwin_opd_logp_grad_problem, base, over)), None)
     assert B.lib.adwin_opd_token_logp_grad(None, None) == B.ADWIN_E_NULL
     assert st(struct_bytes=8) == st(z_dtype=2) == st(dz_dtype=2) == st(temperature=0.0) == B.ADWIN_E_MODE
-    for over in (dict(V=0), dict(T=-1), dict(ld_z=999), dict(ld_dz=999), dict(G=-1), dict(G=B.ADWIN_MAX_GIVEN + 1)):
+    for over in (dict(V=0), dict(T=-1), dict(T=1 << 24), dict(ld_z=999), dict(ld_dz=999), dict(G=-1), dict(G=B.ADWIN_MAX_GIVEN + 1)):
         assert st(**over) == B.ADWIN_E_SHAPE, over
     for name in ("z", "ids", "norm", "g_logp", "entropy", "dz"):
         assert st(**{name: None}) == B.ADWIN_E_NULL, name
