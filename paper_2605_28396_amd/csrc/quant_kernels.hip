@@ -870,7 +870,7 @@ static int product_strips(int64_t tiles, int32_t vocab_tiles, int64_t* turns = n
 // 186 / 155, 192 tokens 196.
 static int product_tile(int64_t T, int32_t V, int pitch) {
   struct Way { int tokens, entries; double first, tile, step; };
-  constexpr Way ways[3] = {{256, 256, 5.0, 6.0, 1.25}, {64, 128, 2.2, 0.5, 0.45}, {128, 128, 2.5, 1.5, 0.62}};
+  constexpr Way ways[3] = {{256, 256, 5.0, 7.0, 1.25}, {64, 128, 2.2, 0.9, 0.45}, {128, 128, 2.5, 1.5, 0.62}};
   int best = 0;
   double least = 0;
   for (int i = 0; i < 3; ++i) {
