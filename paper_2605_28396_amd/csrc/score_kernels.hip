@@ -373,7 +373,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
 }
 
 // One pass over the row, kStep vectors to a thread at a time.  8,192 rows (7,680 of them scored) of V = 151,936 bf16 with 20
-// alternatives: 377 to 390 us over boxes, 6.1 TB/s, without alternatives 365 us.  What bounds it is the read of the logits (a plain read of them 330 to 375 us) and, at
+// alternatives: 368 to 390 us over boxes, 6.1 to 6.3 TB/s, without alternatives 365 us.  What bounds it is the read of the logits (a plain read of them 330 to 375 us) and, at
 // the clock of 2.1 GHz that it gets, the vector unit: 7.5 instructions an entry, 10 with what the alternatives take, busy
 // all the time; without the entropy's two of them it takes 377 us where it took 416.
 // The alternatives ride on the softmax's own maxima: the `top`-th largest of the threads' largest entries is a lower bound of the
