@@ -38,7 +38,10 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 
 // Running sums of one thread, relative to its reference r (in units of the exponent to the base 2).
 struct Sums { float r, s, t, m; };      // s = sum 2^d, t = sum 2^d d, m = largest logit
-constexpr float kNoRef = -1.0e38f;
+// The least reference, and that of no entries.  A reference is a whole number next to some c z, which fp32 gives to a half only as long
+// as |c z| is at most 2^24: beyond, c z - r at the reference's own entry can pass the range of the exponential.  What lies lower
+// (masks of large finite values) is summed as 0 relative to this; pieces whose largest logit lies outside are read again (piece_sums).
+constexpr float kNoRef = -16777216.f;
 // d may reach this before the reference moves.  Exponentials bear more (2^16 is far from the end of fp32), but the largest
 // term's d is rounded where it is summed into t and cancels only there: with 16 the entropy of a peaked row was off by 1e-6.
 constexpr float kSlack = 4.f;
@@ -300,11 +303,12 @@ __device__ __forceinline__ void list_entries(Select& l, int& listed, bool is, co
 }
 
 // The sums relative to the piece's largest logit: 1 <= s, and the entropy log s - t / s has no terms larger than need be.
-// Pieces at the end of the type's range, where c z overflows, are read again, differences first.
+// Pieces whose references do not hold (kNoRef: logits or 1 / temperature of millions, rows at a mask's finite value) are read again,
+// differences first.
 template <typename T>
 __device__ __forceinline__ Sums piece_sums(const Piece<T>& p, const Sums& mine, float c, float (*part)[4]) {
   Sums a = block_sums(mine, part);
-  const bool far = fabsf(a.m * c) > 1.0e30f && fabsf(a.m) < INFINITY;
+  const bool far = fabsf(a.m * c) > -kNoRef && fabsf(a.m) < INFINITY;
   if (a.m == -INFINITY) return a;                    // nothing but masked entries (s = 0) and NaN
   if (!far) {
     const float by = -fmaf(a.m, c, -a.r), f = fast_exp2(by);

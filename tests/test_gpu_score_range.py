@@ -1,0 +1,88 @@
+"""The token-scoring operators at the ends of their ranges: masks of large finite values, logits and temperatures whose quotient passes
+what fp32 counts one by one, scales and derivatives near the ends of the type.  References and tolerances are those of
+test_gpu_score.py, in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from . import test_gpu_score as S
+
+pytestmark = pytest.mark.gpu
+U = S.U
+
+
+@pytest.fixture(scope="module")
+def B():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2605_28396_amd import binding
+    return binding
+
+
+def _f32(x):
+    return float(torch.tensor(x, dtype=torch.float32))
+
+
+def _check_logp(B, out, z, ids, tau, top):
+    """Against the reference in 64 bits, with the tolerances that test_gpu_score.py derives: u S of the sum and 2 u |log p| of a
+    log-probability of any size (S._check_logp counts that part up to 1e30)."""
+    V, ref = z.shape[1], S._reference(z, ids, tau, top)
+    n = math.ceil(V / 256) + 8 + 36 + 2 * (math.log(V) + 1)
+    tol = {k: U * (n + 2 * ref["log_s"].abs()[:, None] + 2 * torch.where(torch.isinf(ref[k]), 0., ref[k]).abs()) for k in ("logp", "top_logp")}
+    tol["entropy"], tol["norm"] = U * n * (2 + 2 * ref["mean"]), U * n * ref["norm"] * torch.tensor([0., 1.])
+    for k, t in tol.items():
+        got, want = out[k].double().cpu(), ref[k]
+        off = torch.where(torch.isinf(want) & (got == want), 0., (got - want).abs())
+        assert torch.all(off <= t), (k, float((off - t).max()))
+    assert torch.equal(out["top_ids"].cpu(), ref["top_ids"])
+
+
+MASKS = [-1e6, -1e7, -1e9, -5e9, -1e10, -1e12, -1e20, -1e30, -1e32, -1e37]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,V", [(8, 300), (8, 9001), (1, 70001), (264, 9001)])
+@pytest.mark.parametrize("tau", [1.0, 0.5, 0.7])
+def test_finite_masks(B, dtype, T, V, tau):
+    """Most entries at a mask's value, whole blocks of a row, all but one, and rows of nothing else: one piece and several."""
+    rows = []
+    for k, mask in enumerate(MASKS):
+        z = S._logits(4, V, dtype, 20 + k)
+        keep = torch.randperm(V, generator=S._gen(V, k))[:max(1, V // 50)]
+        z[0] = torch.full((V,), mask, dtype=dtype).index_copy(0, keep, z[0, keep])
+        z[1, V // 8:V - V // 4] = mask
+        z[2, :V - 1] = mask
+        z[3] = mask
+        rows.append(z)
+    rows = torch.cat(rows)
+    tau = _f32(tau)
+    rows = rows.repeat((max(T, len(rows)) + len(rows) - 1) // len(rows), 1)
+    ids = S._ids(len(rows), 3, V, 7)
+    ids[2, 0] = V - 1
+    for at in range(0, len(rows) - T + 1, T):
+        z, i = rows[at:at + T], ids[at:at + T]
+        out = B.adwin_opd_token_logp(z.cuda(), i.cuda(), temperature=tau, top=9, row_status=True)
+        assert torch.all(out["row_status"] == 0)
+        _check_logp(B, out, z, i, tau, 9)
+        if V > 20000 and at % 5:
+            continue                                               # the gradient is one kernel for all of these
+        gl, gh = torch.randn(T, 3, generator=S._gen(at)), torch.randn(T, generator=S._gen(at, 1))
+        dz = B.adwin_opd_token_logp_grad(z.cuda(), i.cuda(), out["norm"], gl.cuda(), entropy=out["entropy"], g_entropy=gh.cuda(),
+                                         temperature=tau, dz_dtype=B.ADWIN_DT_F32)["dz"].cpu()
+        want, tol = S._grad_reference(z, i, out["norm"].cpu(), out["entropy"].cpu(), gl, gh, tau)
+        assert torch.all((dz.double() - want).abs() <= tol + U * want.abs() * 1.001)
+        assert torch.all((dz != 0).any(dim=1))
+
+
+@pytest.mark.parametrize("T,V", [(3, 500), (2, 20001), (300, 3000)])
+@pytest.mark.parametrize("at,spread,tau", [(0.0, 20.0, 1e-6), (0.0, 20.0, 1e-8), (100.0, 1.0, 1e-8), (0.0, 3.0, 1e-20), (1e6, 10.0, 1.0),
+                                           (3e7, 40.0, 1.0), (3e9, 1e3, 1.0), (-3e9, 1e3, 1.0), (-1e30, 0.0, 1.0), (1e30, 1e24, 1.0), (5.0, 3.0, 1e30)])
+def test_far_logits_and_temperatures(B, T, V, at, spread, tau):
+    """Logits whose quotient by the temperature is far from 0 on either side, with their differences small or large."""
+    z = torch.randn(T, V, generator=S._gen(T, V), dtype=torch.float64).mul_(spread).add_(at).float()
+    tau = _f32(tau)
+    ids = S._ids(T, 2, V, 3)
+    ids[:, 1] = z.argmax(dim=1).int()
+    out = B.adwin_opd_token_logp(z.cuda(), ids.cuda(), temperature=tau, top=5, row_status=True)
+    assert torch.all(out["row_status"] == 0)
+    _check_logp(B, out, z, ids, tau, 5)
