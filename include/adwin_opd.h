@@ -446,7 +446,8 @@ int adwin_opd_quant_rows(const adwin_opd_quant_problem* p, void* hip_stream);
 /* Logits of hidden states under a head kept in 8-bit integers: the rows of h are brought to 8 bits as
  * above (q_h, s_h; in the workspace) and
  *   z[t, v] = s_h[t] W_scale[v] sum_k q_h[t, k] W_q[v, k],
- * the sum exact in 32-bit integers, one rounding of it to fp32 and one of z to its type.  The head is
+ * the sum exact in 32-bit integers; it and its products with one scale and then the other are rounded to fp32, and z to its
+ * type.  No product leaves fp32 (or loses bits below its least normal number) where z does not.  The head is
  * adwin_opd_quant_rows of W [V, H]: laid out once, or whenever the weights change.
  * Limits: 0 <= T < 2^24, 1 <= V <= 2^28, 1 <= H <= ADWIN_QUANT_MAX_H. */
 typedef struct adwin_opd_quant_logits_problem {

@@ -307,6 +307,29 @@ __device__ __forceinline__ u32x4 pack16(const float* y, uint16_t) {
   return u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
 }
 
+// A logit is its integer sum times the token's scale, then the entry's (the product of the scales can leave fp32 where the logit does
+// not).  The first product stays within fp32, as a sum is below 2^30, but for tokens of entries beyond 1e31: their logits are
+// formed and stored 2^-64 times as large, which takes nothing from either type, and a wave that has such tokens raises them at its end.
+constexpr float kHugeScale = 0x1p96f;
+__device__ __forceinline__ float small_scale(float token) { return token >= kHugeScale ? token * 0x1p-64f : token; }
+// z: the wave's first token and first entry; `scale`: from that token on; `rows` of them, `left` entries up to V in pieces of
+// `piece`, `step` apart and `pieces` in number.  The wave's stores have been waited for.
+template <typename T>
+__device__ __forceinline__ void raise_rows(T* z, int64_t ld, const float* scale, int rows, int64_t left, int piece, int step, int pieces) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll 1
+  for (int r = 0; r < rows; ++r) {
+    if (scale[r] < kHugeScale) continue;
+#pragma unroll 1
+    for (int i = 0; i < pieces; ++i)
+#pragma unroll 1
+      for (int q = lane; q < piece; q += 64) {
+        const int64_t v = (int64_t)i * step + q;
+        if (v < left) Entry<T>::put(z + r * ld + v, Entry<T>::one(z + r * ld + v) * 0x1p64f);
+      }
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
   extern __shared__ __align__(16) char lds[];
@@ -350,10 +373,13 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
     swB[kk] = at + wb * (kQBlock / 2);
   }
   float sh[4];                                           // scales of the lane's tokens
+  bool huge = false;                                     // some scale of the wave's tokens is
 #pragma unroll
   for (int fn = 0; fn < 4; ++fn) {
     const int64_t t = t0 + 128 * wb + 32 * fn + (lane & 31);
     sh[fn] = p.h_scale[t < p.T ? t : p.T - 1];
+    huge = huge || __any(sh[fn] >= kHugeScale);
+    sh[fn] = small_scale(sh[fn]);
     asm volatile("" : "+v"(sh[fn]));                     // waited for here, not behind the loads that follow
   }
   // where the lane stores first: token lane / 16 of the wave's, the entries of its chunk; and the tokens from there on
@@ -459,7 +485,7 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
         for (int f = 0; f < kFms; ++f) {
           float y[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) y[e] = acc_read(acc[f0 + f][fn][e]) * (sh[fn] * sv[f0 + f][e]);
+          for (int e = 0; e < 16; ++e) y[e] = acc_read(acc[f0 + f][fn][e]) * sh[fn] * sv[f0 + f][e];
 #pragma unroll
           for (int k = 0; k < 16 / kPer; ++k) {
             const int at = (f * 32 + 16 * half) / kPer + k;
@@ -493,6 +519,11 @@ __global__ __launch_bounds__(256) void quant_tile_kernel(ProductArgs p) {
       }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads that nobody reads may still be writing the LDS
+  if (huge) {
+    const int64_t first = t0 + 128 * wb, v0 = (int64_t)vt0 * kQTile + 128 * wa;
+    raise_rows((T*)p.z + first * p.ld_z + v0, p.ld_z, p.h_scale + first, (int)(p.T - first < 128 ? p.T - first : 128), p.V - v0, 128,
+               kQTile, tiles);
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -586,6 +617,9 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
   i32x4 acc[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) acc[n] = i32x4{0, 0, 0, 0};
+  bool huge = false;                                     // some scale of the tokens is
+#pragma unroll
+  for (int n = 0; n < NT; ++n) huge = huge || __any(sh[n] >= kHugeScale);
   int k = 0, g = g0 + wave;
   const char* frag = lds + lane * 16 + turn * (2 * NT * 1024);
   for (int at = 0; at < total; at += kAhead) {
@@ -608,8 +642,14 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const int64_t t = n * 16 + (lane & 15);
-          const float y[4] = {(float)acc[n][0] * (sh[n] * sv.x), (float)acc[n][1] * (sh[n] * sv.y),
-                              (float)acc[n][2] * (sh[n] * sv.z), (float)acc[n][3] * (sh[n] * sv.w)};
+          float first = sh[n];
+          if (huge) first = small_scale(sh[n]);
+          float y[4] = {(float)acc[n][0] * first * sv.x, (float)acc[n][1] * first * sv.y,
+                        (float)acc[n][2] * first * sv.z, (float)acc[n][3] * first * sv.w};
+          if (huge && sh[n] >= kHugeScale) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] *= 0x1p64f;
+          }
           if (t < p.T) {
             T* z = (T*)p.z + t * p.ld_z + v;
             if (p.whole && v + 4 <= p.V) put_entries<false>(z, y, true);
@@ -683,10 +723,13 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
     swB[kk] = at + Tile::kBlockA + wb * (32 * FN * 128);
   }
   float sh[FN];
+  bool huge = false;                                     // some scale of the wave's tokens is
 #pragma unroll
   for (int fn = 0; fn < FN; ++fn) {
     const int64_t t = 32 * FN * wb + 32 * fn + (lane & 31);
     sh[fn] = p.h_scale[t0 + (t < T_left ? t : T_left - 1)];
+    huge = huge || __any(sh[fn] >= kHugeScale);
+    sh[fn] = small_scale(sh[fn]);
     asm volatile("" : "+v"(sh[fn]));                     // waited for here
   }
 
@@ -795,7 +838,7 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
         for (int f = 0; f < kFms; ++f) {
           float y[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) y[e] = (float)acc[f0 + f][fn][e] * (sh[fn] * sv[f0 + f][e]);
+          for (int e = 0; e < 16; ++e) y[e] = (float)acc[f0 + f][fn][e] * sh[fn] * sv[f0 + f][e];
 #pragma unroll
           for (int k = 0; k < 16 / kPer; ++k) {
             const int at = (f * 32 + 16 * half) / kPer + k;
@@ -821,6 +864,12 @@ __global__ __launch_bounds__(256) void quant_mid_kernel(ProductArgs p) {
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // loads that nobody reads may still be writing the LDS
+  if (huge) {
+    constexpr int kRows = 32 * FN;
+    const int64_t first = t0 + kRows * wb, v0 = (int64_t)vt0 * Tile::kEntries + 64 * wa;
+    raise_rows((T*)p.z + first * p.ld_z + v0, p.ld_z, p.h_scale + first, (int)(p.T - first < kRows ? p.T - first : kRows), p.V - v0, 64,
+               Tile::kEntries, tiles);
+  }
 }
 
 static int check_quant(const adwin_opd_quant_problem* p) {

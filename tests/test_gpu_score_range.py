@@ -86,3 +86,33 @@ def test_far_logits_and_temperatures(B, T, V, at, spread, tau):
     out = B.adwin_opd_token_logp(z.cuda(), ids.cuda(), temperature=tau, top=5, row_status=True)
     assert torch.all(out["row_status"] == 0)
     _check_logp(B, out, z, ids, tau, 5)
+
+
+# few tokens, the tiles of 128 entries, those of 256
+@pytest.mark.parametrize("T,V,H", [(3, 500, 300), (40, 1000, 256), (100, 3001, 512), (300, 9001, 384), (1100, 33001, 1500)])
+@pytest.mark.parametrize("z_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("token,entry", [(1e-20, 1e-20), (1e-30, 1e-7), (1e22, 1e22), (1e35, 1e-30), (1e-30, 1e35)])
+def test_product_of_far_scales(B, T, V, H, z_dtype, token, entry):
+    """Scales whose product leaves fp32, or all but does, with logits inside it, zero sums and logits beyond it: tokens and entries of
+    such magnitudes among ordinary ones."""
+    g = torch.Generator("cuda").manual_seed(T)
+    h = torch.randn(T, H, generator=g, device="cuda")
+    W = torch.randn(V, H, generator=g, device="cuda") * 0.05
+    h[::2] *= token
+    W[::3] *= entry
+    h[0, :] = 0
+    h[0, H // 2:] = token                                          # times an entry with zeros there: a sum of 0
+    W[3, H // 2:] = 0
+    W[6] = 0
+    (qh, sh, _), (qW, sW, _) = S._quantised(h.cpu()), S._quantised(W.cpu())
+    got = B.QuantHead(W).logits(h, z_dtype=B._DTYPE[z_dtype])
+    least = 2.0 ** -149 if z_dtype == torch.float32 else 2.0 ** -133
+    qh, sh, qW, sW = (x.cuda().double() for x in (qh, sh, qW, sW))
+    for lo in range(0, V, 16384):
+        want = (qh @ qW[lo:lo + 16384].t().contiguous()) * sh[:, None] * sW[lo:lo + 16384]
+        beyond = want.abs() * (1 + 2.0 ** -7) > torch.finfo(z_dtype).max
+        tol = want.abs() * (3.01 * U + (torch.finfo(z_dtype).eps / 2 if z_dtype != torch.float32 else 0)) + 2 * least
+        z = got[:, lo:lo + 16384].double()
+        assert torch.all(((z - want).abs() <= tol) | beyond) and not torch.any(torch.isnan(z))
+        assert torch.all(z[beyond].abs() >= torch.finfo(z_dtype).max * (1 - 2.0 ** -6))
+    assert torch.all(got[0, 3] == 0) and torch.all(got[:, 6] == 0)
