@@ -594,7 +594,7 @@ struct LogpGradArgs {
 struct GradRow {
   float m, c, per_s, log_s, a, gh, H, per_temperature;
   __device__ __forceinline__ float plain(float z) const {       // times temperature
-    const float d = fmaxf((z - m) * c, kNegBig);
+    const float d = fmaxf((z - m) * c, -256.f);                 // p = 0 from there on; masked entries times gh stay finite
     const float p = fast_exp2(d) * per_s;
     return -p * fmaf(gh, fmaf(d, kLn2, H - log_s), a);
   }

@@ -116,3 +116,20 @@ def test_product_of_far_scales(B, T, V, H, z_dtype, token, entry):
         assert torch.all(((z - want).abs() <= tol) | beyond) and not torch.any(torch.isnan(z))
         assert torch.all(z[beyond].abs() >= torch.finfo(z_dtype).max * (1 - 2.0 ** -6))
     assert torch.all(got[0, 3] == 0) and torch.all(got[:, 6] == 0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,V", [(4, 700), (3, 30001)])
+def test_large_derivatives_of_masked_rows(B, dtype, T, V):
+    """Derivatives by the entropy as a scaled loss has them: a masked entry's gradient is 0, not 0 times inf."""
+    z, ids = S._logits(T, V, dtype, 1), S._ids(T, 2, V, 2)
+    z[:, V // 2:] = -math.inf
+    z[1, :V // 2 - 1] = torch.finfo(dtype).min
+    z[2, ::3] = -1e10
+    f = B.adwin_opd_token_logp(z.cuda(), ids.cuda())
+    for size in (1.0, 1e9, 1e20, 1e33):
+        gl, gh = torch.randn(T, 2, generator=S._gen(T)) * size, torch.randn(T, generator=S._gen(V)) * size
+        dz = B.adwin_opd_token_logp_grad(z.cuda(), ids.cuda(), f["norm"], gl.cuda(), entropy=f["entropy"], g_entropy=gh.cuda(),
+                                         dz_dtype=B.ADWIN_DT_F32)["dz"].cpu().double()
+        want, tol = S._grad_reference(z, ids, f["norm"].cpu(), f["entropy"].cpu(), gl, gh, 1.0)
+        assert torch.all((dz - want).abs() <= tol + U * want.abs() * 1.001), size
