@@ -470,7 +470,9 @@ def _on_stream(call):
     def on(*args, stream=None, **kw):
         if stream is None:
             return call(*args, **kw)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        if isinstance(stream, int):                # 0 is the default stream, which ExternalStream does not take
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+        with torch.cuda.stream(stream):
             return call(*args, **kw)
     return on
 
