@@ -493,12 +493,17 @@ def _flat(name, x, dtype, *shape):
 
 
 @_on_stream
-def adwin_opd_quant_rows(x, row_status=False) -> dict:
-    """Rows x [N, H] (bf16, fp32) as 8-bit integers: `q` [N, ADWIN_QUANT_PITCH(H)], `scale` [N]."""
+def adwin_opd_quant_rows(x, row_status=False, q=None, scale=None) -> dict:
+    """Rows x [N, H] (bf16, fp32) as 8-bit integers: `q` [N, ADWIN_QUANT_PITCH(H)], `scale` [N].  q, scale: where they go;
+    else new tensors."""
     ld = _rows("x", x)
     N, H = x.shape
-    q = torch.empty(N, ADWIN_QUANT_PITCH(H), dtype=torch.int8, device=x.device)
-    scale = torch.empty(N, dtype=torch.float32, device=x.device)
+    if q is None:
+        q = torch.empty(N, ADWIN_QUANT_PITCH(H), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(N, dtype=torch.float32, device=x.device)
+    _flat("q", q, torch.int8, N, ADWIN_QUANT_PITCH(H))
+    _flat("scale", scale, torch.float32, N)
     out = {"q": q, "scale": scale}
     if row_status:
         out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
@@ -546,13 +551,20 @@ def adwin_opd_quant_logits(h, W_q, W_scale, z_dtype=ADWIN_DT_BF16, z=None, row_s
 
 
 class QuantHead:
-    """A head W [V, H] kept in 8-bit integers; set(W) lays it out again after its weights have changed."""
+    """A head W [V, H] kept in 8-bit integers; set(W) lays it out again after its weights have changed, in the same arrays
+    unless W has other sizes, so that a captured graph goes on with the new weights.  (Products under way on another stream
+    read these arrays: the caller orders them.)"""
+
+    W_q = W_scale = None
 
     def __init__(self, W, stream=None):
         self.set(W, stream)
 
     def set(self, W, stream=None):
-        out = adwin_opd_quant_rows(W, stream=stream)
+        kept = {}
+        if self.W_q is not None and W.shape == (self.W_q.shape[0], self.H) and W.device == self.W_q.device:
+            kept = {"q": self.W_q, "scale": self.W_scale}
+        out = adwin_opd_quant_rows(W, stream=stream, **kept)
         self.W_q, self.W_scale, self.H = out["q"], out["scale"], int(W.shape[1])
 
     def logits(self, h, z_dtype=ADWIN_DT_BF16, z=None, stream=None):

@@ -26,3 +26,33 @@ def test_stream_zero_is_the_default_stream(B, monkeypatch):
         for s in (None, 0, torch.cuda.default_stream(), side, side.cuda_stream):
             B.adwin_opd_token_logp(z, ids, stream=s)
     assert got == [side.cuda_stream, None, None, side.cuda_stream, side.cuda_stream]
+
+
+def test_a_head_is_laid_out_again_in_its_arrays(B):
+    """A captured product goes on with the weights that set() brings; other sizes get arrays of their own."""
+    V, H, T = 3001, 200, 20
+    W = [torch.randn(V, H, generator=S._gen(k)).cuda() for k in range(3)]
+    h = torch.randn(T, H, generator=S._gen(9)).cuda()
+    want = [B.QuantHead(w).logits(h) for w in W]
+    head = B.QuantHead(W[0])
+    at = head.W_q.data_ptr(), head.W_scale.data_ptr()
+    z = torch.empty_like(want[0])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        head.logits(h, z=z)
+    for k in (1, 2, 0, 1):
+        head.set(W[k])
+        assert (head.W_q.data_ptr(), head.W_scale.data_ptr()) == at
+        z.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(z, want[k]), k
+    for other in (W[0][:, :100].contiguous(), W[0][:5], W[0][:, :199]):
+        head.set(other)
+        assert torch.equal(head.logits(h[:, :other.shape[1]]), B.QuantHead(other).logits(h[:, :other.shape[1]]))
+    with pytest.raises(ValueError):
+        B.adwin_opd_quant_rows(W[0], q=torch.empty(V, H, dtype=torch.int8, device="cuda"))
+    with pytest.raises(ValueError):
+        B.adwin_opd_quant_rows(W[0], scale=torch.empty(V, device="cuda").half())
