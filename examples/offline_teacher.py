@@ -9,7 +9,8 @@ alternatives, its loss is the teacher's cross-entropy on them, over its least va
     sum_k e^{t_k} (t_k - q_k) - bonus H,
 
 whose derivatives by q and H go back through adwin_opd_token_logp_grad to the student's logits, and from there to its
-hidden states and head.  Rows outside the windows carry the id -1: they are not scored and get no gradient.
+hidden states and head.  Rows outside the windows carry the id -1: they are not scored and get no gradient.  So do rows
+whose hidden states hold an inf or NaN, the teacher's or the student's.
 
     python examples/offline_teacher.py [--rollouts 8] [--length 512] [--vocab 32000] [--steps 20]
 """
@@ -37,14 +38,16 @@ def admitted_ids(ids, offsets, window):
 
 def teacher_answers(head: B.QuantHead, h_t, ids, top=20, slab=2048):
     """What training needs of the teacher: `logp` [T] of the sampled tokens, `top_ids` and `top_logp` [T, top]."""
+    if bool((head.row_status != 0).any()):
+        raise ValueError(f"weights of {int((head.row_status != 0).sum())} entries of the teacher's head hold an inf or NaN")
     T, V = h_t.shape[0], head.W_q.shape[0]
     z = torch.empty(min(slab, T), (V + 7) & ~7, dtype=torch.bfloat16, device=h_t.device)[:, :V]
     parts = []
     for lo in range(0, T, slab):
         rows = slice(lo, min(lo + slab, T))
         here = z[:rows.stop - lo]
-        head.logits(h_t[rows], z=here)
-        parts.append(B.adwin_opd_token_logp(here, ids[rows], top=top))
+        _, status = head.logits(h_t[rows], z=here, row_status=True)
+        parts.append(B.adwin_opd_token_logp(here, torch.where(status == 0, ids[rows], -1), top=top))
     return {k: torch.cat([p[k] for p in parts]) for k in ("logp", "top_ids", "top_logp")}
 
 
@@ -53,7 +56,7 @@ def student_step(h_s, W_s, answers, bonus=0.0):
     z = h_s @ W_s.t()
     ids, t = answers["top_ids"], answers["top_logp"]
     out = B.adwin_opd_token_logp(z, ids)
-    scored = ids >= 0
+    scored = (ids >= 0) & (out["norm"][:, 1:] > 0)          # norm is 0, 0 where the student's logits are not finite
     count = scored.any(dim=1).sum().clamp(min=1)
     p_t = torch.where(scored, t.exp(), 0.)
     loss = ((p_t * (t - out["logp"])).sum() - bonus * out["entropy"].sum()) / count
@@ -61,7 +64,7 @@ def student_step(h_s, W_s, answers, bonus=0.0):
     g_entropy = torch.full_like(out["entropy"], -bonus) / count
     # z is not needed any more: its gradient takes its place
     dz = B.adwin_opd_token_logp_grad(z, ids, out["norm"], g_logp, entropy=out["entropy"], g_entropy=g_entropy, dz=z)["dz"]
-    return loss, dz @ W_s, dz.t() @ h_s
+    return loss, dz @ W_s, dz.t() @ h_s.masked_fill(~scored.any(dim=1, keepdim=True), 0)      # 0 times NaN is none
 
 
 def main():

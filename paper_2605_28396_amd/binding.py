@@ -494,8 +494,8 @@ def _flat(name, x, dtype, *shape):
 
 @_on_stream
 def adwin_opd_quant_rows(x, row_status=False, q=None, scale=None) -> dict:
-    """Rows x [N, H] (bf16, fp32) as 8-bit integers: `q` [N, ADWIN_QUANT_PITCH(H)], `scale` [N].  q, scale: where they go;
-    else new tensors."""
+    """Rows x [N, H] (bf16, fp32) as 8-bit integers: `q` [N, ADWIN_QUANT_PITCH(H)], `scale` [N], and `row_status` [N] if
+    wanted.  q, scale, row_status: where they go; else new tensors."""
     ld = _rows("x", x)
     N, H = x.shape
     if q is None:
@@ -505,8 +505,11 @@ def adwin_opd_quant_rows(x, row_status=False, q=None, scale=None) -> dict:
     _flat("q", q, torch.int8, N, ADWIN_QUANT_PITCH(H))
     _flat("scale", scale, torch.float32, N)
     out = {"q": q, "scale": scale}
-    if row_status:
+    if row_status is True:
         out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
+    elif isinstance(row_status, torch.Tensor):
+        _flat("row_status", row_status, torch.int32, N)
+        out["row_status"] = row_status
     p = adwin_opd_quant_problem(C.sizeof(adwin_opd_quant_problem), N, ld, H, _DTYPE[x.dtype], x.data_ptr(), q.data_ptr(),
                                 scale.data_ptr(), _ptr(out.get("row_status")))
     _check(lib.adwin_opd_quant_rows(p, _stream_handle(None)))
@@ -553,9 +556,12 @@ def adwin_opd_quant_logits(h, W_q, W_scale, z_dtype=ADWIN_DT_BF16, z=None, row_s
 class QuantHead:
     """A head W [V, H] kept in 8-bit integers; set(W) lays it out again after its weights have changed, in the same arrays
     unless W has other sizes, so that a captured graph goes on with the new weights.  (Products under way on another stream
-    read these arrays: the caller orders them.)"""
+    read these arrays: the caller orders them.)
 
-    W_q = W_scale = None
+    `row_status` [V]: ADWIN_DEV_NONFINITE where an entry's weights hold an inf or NaN.  Its logits are 0 then, which nothing
+    downstream can tell from an answer: look at it once per set()."""
+
+    W_q = W_scale = row_status = None
 
     def __init__(self, W, stream=None):
         self.set(W, stream)
@@ -563,12 +569,15 @@ class QuantHead:
     def set(self, W, stream=None):
         kept = {}
         if self.W_q is not None and W.shape == (self.W_q.shape[0], self.H) and W.device == self.W_q.device:
-            kept = {"q": self.W_q, "scale": self.W_scale}
-        out = adwin_opd_quant_rows(W, stream=stream, **kept)
-        self.W_q, self.W_scale, self.H = out["q"], out["scale"], int(W.shape[1])
+            kept = {"q": self.W_q, "scale": self.W_scale, "row_status": self.row_status}
+        out = adwin_opd_quant_rows(W, stream=stream, **{"row_status": True, **kept})
+        self.W_q, self.W_scale, self.row_status, self.H = out["q"], out["scale"], out["row_status"], int(W.shape[1])
 
-    def logits(self, h, z_dtype=ADWIN_DT_BF16, z=None, stream=None):
-        return adwin_opd_quant_logits(h, self.W_q, self.W_scale, z_dtype=z_dtype, z=z, stream=stream)["z"]
+    def logits(self, h, z_dtype=ADWIN_DT_BF16, z=None, stream=None, row_status=False):
+        """Logits [T, V]; with row_status also [T] that says which rows of h held an inf or NaN: their logits are 0, and what
+        scores them has to leave them out."""
+        out = adwin_opd_quant_logits(h, self.W_q, self.W_scale, z_dtype=z_dtype, z=z, row_status=row_status, stream=stream)
+        return (out["z"], out["row_status"]) if row_status else out["z"]
 
 
 def adwin_opd_token_logp_workspace_bytes(p: adwin_opd_logp_problem) -> int:
