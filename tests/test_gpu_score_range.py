@@ -133,3 +133,50 @@ def test_large_derivatives_of_masked_rows(B, dtype, T, V):
                                          dz_dtype=B.ADWIN_DT_F32)["dz"].cpu().double()
         want, tol = S._grad_reference(z, ids, f["norm"].cpu(), f["entropy"].cpu(), gl, gh, 1.0)
         assert torch.all((dz - want).abs() <= tol + U * want.abs() * 1.001), size
+
+
+def _least_us(call, n=20, times=5):
+    """Microseconds of a call among others, the least of several measurements."""
+    call()
+    us = []
+    for _ in range(times):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(n):
+            call()
+        b.record()
+        torch.cuda.synchronize()
+        us.append(a.elapsed_time(b) * 1e3 / n)
+    return min(us)
+
+
+@pytest.mark.parametrize("T,V,top,finite", [(264, 30011, 64, 100), (1000, 100003, 20, 500)])
+def test_heavily_masked_rows_are_selected_in_one_pass(B, T, V, top, finite):
+    """Alternatives of rows that a mask leaves few entries of, more than `top` all the same: no slower than of whole rows by a
+    factor (going through the rows again, round by round, took eight times as long)."""
+    z = torch.randn(T, V, generator=torch.Generator("cuda").manual_seed(T), device="cuda").bfloat16()
+    masked = torch.full_like(z, -math.inf)
+    keep = torch.randperm(V, generator=S._gen(V))[:finite].cuda()
+    masked[:, keep] = z[:, keep]
+    ids = keep[:1].int().repeat(T, 1)
+    out = B.adwin_opd_token_logp(masked, ids, top=top)
+    few = T // 40
+    _check_logp(B, {k: v[:few] for k, v in out.items()}, masked[:few].cpu(), ids[:few].cpu(), 1.0, top)
+    assert _least_us(lambda: B.adwin_opd_token_logp(masked, ids, top=top)) <= 3 * _least_us(lambda: B.adwin_opd_token_logp(z, ids, top=top))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,V", [(5, 400), (3, 790), (300, 600), (300, 1560), (264, 9001), (2, 70001)])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_few_finite_entries(B, dtype, T, V, top):
+    """Rows with fewer finite entries than alternatives, as many, and some more; with and without one wave that has them all."""
+    z = torch.full((T, V), -math.inf)
+    for t in range(T):
+        n = (0, top - 1, top, top + 1, 3 * top)[t % 5] + (t % 5 == 0)
+        at = torch.randperm(V if t % 2 else max(V // 5, 3 * top), generator=S._gen(t, V))[:n]
+        z[t, at.clamp(max=V - 1)] = torch.randn(len(at), generator=S._gen(t))
+    z = z.to(dtype)
+    ids = z.argmax(dim=1).int()[:, None].contiguous()
+    out = B.adwin_opd_token_logp(z.cuda(), ids.cuda(), top=top, row_status=True)
+    assert torch.equal(out["row_status"].cpu() != 0, torch.isinf(z).all(dim=1))
+    _check_logp(B, out, z, ids, 1.0, top)
