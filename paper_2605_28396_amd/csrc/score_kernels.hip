@@ -43,18 +43,14 @@ struct Sums { float r, s, t, m; };      // s = sum 2^d, t = sum 2^d d, m = large
 // (masks of large finite values) is summed as 0 relative to this; pieces whose largest logit lies outside are read again (piece_sums).
 constexpr float kNoRef = -16777216.f;
 // d may reach this before the reference moves.  Exponentials bear more (2^16 is far from the end of fp32), but the largest
-// term's d is rounded where it is summed into t and cancels only there: with 16 the entropy of a peaked row was off by 1e-6.
+// term's d is rounded where it is summed into t and cancels only there: with 16 the entropy of rows with one likely token was off by 2.6e-6
+// at most (fp32 7.1e-6) where it is 8e-7 (1.3e-6) with 4.
 constexpr float kSlack = 4.f;
 // References are whole numbers, so that moving and merging sums multiplies by exact powers of two (with the threads' largest
-// exponents themselves, the roundings of their differences were the same for all terms of a thread: s was off by 9e-7 where it is 1e-7 now).
+// exponents themselves, the roundings of their differences were the same for all terms of a thread).
 __device__ __forceinline__ float ref_of(float m, float c) { return ceilf(m * c); }
 __device__ __forceinline__ Sums no_sums() { return {kNoRef, 0.f, 0.f, -INFINITY}; }
 
-__device__ __forceinline__ void add_one(Sums& a, float z, float c) {
-  const float d = fmaf(z, c, -a.r), e = fast_exp2(d);
-  a.s += e;
-  a.t = fmaf(e, fmaxf(d, kNegBig), a.t);     // a masked entry is 0 times something finite
-}
 __device__ __forceinline__ void move_ref(Sums& a, float r) {
   const float by = a.r - r, f = fast_exp2(by);
   a.t = f * fmaf(a.s, fmaxf(by, kNegBig), a.t);
@@ -67,7 +63,9 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(x), "v"(y), "v"(z));
   return m;
 }
-// returns the largest of x
+// Returns the largest of x.  The terms of a vector are summed first: bf16 logits and whole-number references give few different terms, whose
+// roundings in one sum per thread, 594 terms long at V = 151,936, were the same in all threads and did not average out: s was off by 8.8e-6
+// at most where all logits are equal, by 3.3e-6 where a likely token comes early, and is by 1.1e-6 and 4.5e-7 so (fp32 2.2e-6, 7.3e-7).
 template <int N>
 __device__ __forceinline__ float add_entries(Sums& a, const float (&x)[N], float c) {
   float m = x[0];
@@ -77,8 +75,19 @@ __device__ __forceinline__ float add_entries(Sums& a, const float (&x)[N], float
   if constexpr (N > 1) m = max3(m, x[N - 1], x[N - 1]);
   a.m = max3(a.m, m, m);
   if (m * c > a.r + kSlack) move_ref(a, ref_of(m, c));
+  float e[N], t = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) add_one(a, x[i], c);
+  for (int i = 0; i < N; ++i) {
+    const float d = fmaf(x[i], c, -a.r);
+    e[i] = fast_exp2(d);
+    t = fmaf(e[i], fmaxf(d, kNegBig), t);            // a masked entry is 0 times something finite
+  }
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2)
+#pragma unroll
+    for (int i = 0; i < n; ++i) e[i] += e[i + n];
+  a.s += e[0];
+  a.t += t;
   return m;
 }
 // Sums over the workgroup.  All move to the largest reference first, which multiplies them by powers of two.
@@ -323,17 +332,19 @@ __device__ __forceinline__ Sums piece_sums(const Piece<T>& p, const Sums& mine, 
   }
   __syncthreads();
   Sums b = {0.f, 0.f, 0.f, a.m};
-  auto add = [&](float z) {
+  auto add = [&](float z, float& s, float& t) {
     const float d = (z - a.m) * c, e = fast_exp2(d);
-    b.s += e;
-    b.t = fmaf(e, fmaxf(d, kNegBig), b.t);
+    s += e;
+    t = fmaf(e, fmaxf(d, kNegBig), t);
   };
-  if ((int)threadIdx.x < p.edge) add(Entry<T>::one(p.row.p + p.row.edge_index(threadIdx.x)));
+  if ((int)threadIdx.x < p.edge) add(Entry<T>::one(p.row.p + p.row.edge_index(threadIdx.x)), b.s, b.t);
   for (int i = p.v0 + threadIdx.x; i < p.v1; i += kThreads) {
-    float x[Entry<T>::kPerVec];
+    float x[Entry<T>::kPerVec], s = 0.f, t = 0.f;
     Entry<T>::unpack(p.row.vec(i), x);
 #pragma unroll
-    for (int e = 0; e < Entry<T>::kPerVec; ++e) add(x[e]);
+    for (int e = 0; e < Entry<T>::kPerVec; ++e) add(x[e], s, t);
+    b.s += s;
+    b.t += t;
   }
   return block_sums(b, part);
 }

@@ -180,3 +180,36 @@ def test_few_finite_entries(B, dtype, T, V, top):
     out = B.adwin_opd_token_logp(z.cuda(), ids.cuda(), top=top, row_status=True)
     assert torch.equal(out["row_status"].cpu() != 0, torch.isinf(z).all(dim=1))
     _check_logp(B, out, z, ids, 1.0, top)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [151936, 40003])
+@pytest.mark.parametrize("rows", ["equal", "policy", "peaked early"])
+def test_sums_of_long_rows(B, dtype, V, rows):
+    """s and log p of rows that a workgroup sums whole, to the roundings that there are: n_v vectors of N entries to a thread, whose
+    terms are summed first (log2 N of them one after the other), the edge, six steps over the lanes and three over the waves; a
+    term itself is off by u (2 + 2 |x| + 3.5), the reference at most 5 above it, and the move to the largest logit by 6.5 u more.  Sums of
+    n equal terms are off by u (n + 1) / 2 only, as the partial sums are smaller than the last one."""
+    T, N = 264, 8 if dtype == torch.bfloat16 else 4
+    g = torch.Generator("cuda").manual_seed(V)
+    if rows == "equal":
+        z = (torch.arange(T, device="cuda") / 37 - 3)[:, None].repeat(1, V)
+    else:
+        z = torch.randn(T, V, generator=g, device="cuda") * 1.8
+        at = torch.randint(0, V if rows == "policy" else 2000, (T, 8), generator=g, device="cuda")
+        z.scatter_(1, at, (0.3 + 0.9 * torch.rand(T, 8, generator=g, device="cuda")) * (math.log(V) + 2) + 4 * (rows != "policy"))
+    z = z.to(dtype)
+    ids = torch.randint(0, V, (T, 2), generator=g, device="cuda", dtype=torch.int32)
+    out = B.adwin_opd_token_logp(z, ids)
+    x = z.double()
+    x -= x.amax(dim=1, keepdim=True)
+    e = x.exp()
+    s = e.sum(dim=1)
+    mean = -(e * x).sum(dim=1) / s
+    vectors = math.ceil(V / (256 * N))
+    chain = (vectors + 1) / 2 if rows == "equal" else vectors
+    tol = U * (chain + math.log2(N) + 1 + 9 + 12 + 2 * mean)
+    assert torch.equal(out["norm"][:, 0], z.float().amax(dim=1))
+    assert torch.all((out["norm"][:, 1].double() / s - 1).abs() <= tol)
+    logp = x.gather(1, ids.long()) - torch.log(s)[:, None]
+    assert torch.all((out["logp"].double() - logp).abs() <= tol[:, None] + U * (2 * logp.abs() + 2 * torch.log(s)[:, None].abs()))
