@@ -1,5 +1,6 @@
 // Rows to 8-bit integers, and the product of two arrays of such rows.
 #include "fused_shared.h"
+#include "product_rule.h"
 #include "score_shared.h"
 
 namespace adwin {
@@ -897,40 +898,6 @@ struct QuantLayout {
   }
 };
 
-// Strips of the vocabulary for `tiles` token tiles: one workgroup occupies a compute unit, so that what counts is the number of
-// rounds times the tiles of the longest strip (*turns); of as good ones in a single round the most.
-static int product_strips(int64_t tiles, int32_t vocab_tiles, int64_t* turns = nullptr) {
-  int64_t best = 0;
-  int strips = 1;
-  for (int s = 1; s <= vocab_tiles && s <= 256; ++s) {
-    const int64_t cost = (tiles * s + 255) / 256 * ((vocab_tiles + s - 1) / s);
-    if (best == 0 || cost < best || (cost == best && tiles * s <= 256)) { best = cost; strips = s; }
-  }
-  if (turns) *turns = best;
-  return strips;
-}
-
-// The tile of a product: 64 or 128 tokens x 128 entries (1, 2), or 256 x 256 (0).  What a call takes is near
-// first + turns (tile + k-steps step), turns being the tiles that the busiest compute unit goes through one after the other; the
-// numbers (us) are fitted to the calls below, whose times they give to 15 % and whose order they keep.  us, 256 x 256 / 128 x 128 / 64 x 128
-// (with 5 for the tokens' integers): 1,000 tokens, V = 2,000, H = 1024 25.8 / 14.3 / 12.0, H = 4096 54 / 30 / 25; V = 8,000,
-// H = 2048 38 / 31 / 37; 701 tokens, V = 11,907, H = 632 24.2 / 22.2 / 24.5; 400 tokens, V = 32,000, H = 1024 27.5 / 31.5 / 37.4; 600 tokens,
-// V = 50,000 63 / 58 / 76; 2,048 tokens, V = 16,000, H = 2048 77 / 94 / 118; 300 tokens, V = 151,936, H = 1024 98 / 93 / 115, 100 tokens, H = 4096
-// 186 / 155, 192 tokens 196.
-static int product_tile(int64_t T, int32_t V, int pitch) {
-  struct Way { int tokens, entries; double first, tile, step; };
-  constexpr Way ways[3] = {{256, 256, 5.0, 7.0, 1.25}, {64, 128, 2.2, 0.9, 0.45}, {128, 128, 2.5, 1.5, 0.62}};
-  int best = 0;
-  double least = 0;
-  for (int i = 0; i < 3; ++i) {
-    int64_t turns;
-    product_strips((T + ways[i].tokens - 1) / ways[i].tokens, (V + ways[i].entries - 1) / ways[i].entries, &turns);
-    const double us = ways[i].first + (double)turns * (ways[i].tile + pitch / 128 * ways[i].step);
-    if (i == 0 || us < least) { least = us; best = i; }
-  }
-  return best;
-}
-
 // Groups of 16 tokens of the kernel for few tokens, 0 where tiles serve the call: as many as fit the LDS, at most 4, but for more than
 // two where one or two tiles of 128 entries to a compute unit spread as well and are filled by the tokens.  us, few / tiles: 1 token,
 // H = 1024, V = 1,000 7.5 / 10.2, V = 151,936 30.5 / 33.2, H = 4096, V = 4,000 11.5 / 19.3; 16 tokens, H = 4096, V = 16,000 21.4 / 21.1,
@@ -1051,7 +1018,7 @@ extern "C" int adwin_opd_quant_logits(const adwin_opd_quant_logits_problem* p, v
     ADWIN_HIP_TRY(p->z_dtype == ADWIN_DT_BF16 ? launch_few<uint16_t>(a, few, stream) : launch_few<float>(a, few, stream));
     return ADWIN_OK;
   }
-  if (const int way = product_tile(p->T, p->V, a.pitch)) {
+  if (const int way = product_tile(p->T, p->V, a.pitch, (int)size)) {
     const bool bf16 = p->z_dtype == ADWIN_DT_BF16;
     ADWIN_HIP_TRY(way == 1 ? (bf16 ? launch_mid<uint16_t, 1>(a, stream) : launch_mid<float, 1>(a, stream))
                            : (bf16 ? launch_mid<uint16_t, 2>(a, stream) : launch_mid<float, 2>(a, stream)));
