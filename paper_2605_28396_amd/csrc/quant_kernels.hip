@@ -193,8 +193,8 @@ struct ProductArgs {
 // more, the tokens behind those of sub-step 3 into the one that this step has finished.  The one barrier of a step stands before
 // its last sub-step, when every fragment of the step is in registers, and that sub-step's MFMAs cover the reads of the
 // next step's first fragments.  The order of the instructions is pinned, a read, a load or a piece of bookkeeping behind each MFMA.
-// 4,096 tokens, V = 151,936, H = 4096, bf16 logits: 2.14 to 2.22 ms over boxes, 2.3 to 2.4 POP/s, where the library's 8-bit product
-// reaches 1.85 and its bf16 one 1.3.  The matrix pipe is busy 66 % of the cycles at 1.67 GHz (power); the epilogue, which
+// 4,096 tokens, V = 151,936, H = 4096, bf16 logits: 2.11 to 2.28 ms over machines, 2.2 to 2.4 POP/s, where the library's 8-bit product
+// reaches 1.85 and its bf16 one 1.3.  The matrix pipe is busy 66 % of the cycles at 1.57 to 1.67 GHz (power); the epilogue, which
 // nothing overlaps with one wave to a SIMD, takes 15 % (half of it the arithmetic, half the stores, which all compute units issue at about the
 // same time; workgroups begun at different times: 2 % slower), the k-steps wait 14 % for loads.  How token tiles and strips are
 // grouped over the XCDs makes no difference (1, 2, 4 and 8 token tiles within 0.6 %).
@@ -676,7 +676,7 @@ __global__ __launch_bounds__(kFewThreads) void quant_few_kernel(ProductArgs p) {
 // latency, and what counts is how much is under way: a ring of kStages
 // k-steps (128 bytes of 128 rows of W and of the tokens), all but one of them loading.  2 x 2 waves of 64 x 32 FN; operands,
 // fragments and their places in the LDS as in the kernel of many tokens.  V = 151,936, H = 4096: 64 tokens 145 us with the rows'
-// integers (4.4 TB/s), 128 tokens 165 us; 1,187 tiles are 4.6 rounds of 256 compute units and run as 5.
+// integers (4.4 TB/s), 128 tokens 168 to 179 us; 1,187 tiles are 4.6 rounds of 256 compute units and run as 5.
 // ---------------------------------------------------------------------------------------
 template <int FN>
 struct MidTile {

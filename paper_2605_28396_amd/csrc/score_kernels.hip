@@ -393,7 +393,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int64_t row, const
 }
 
 // One pass over the row, kStep vectors to a thread at a time.  8,192 rows (7,680 of them scored) of V = 151,936 bf16 with 20
-// alternatives: 368 to 390 us over boxes, 6.1 to 6.3 TB/s, without alternatives 365 us.  What bounds it is the read of the logits (a plain read of them 330 to 375 us) and, at
+// alternatives: 368 to 390 us over machines, 6.0 to 6.3 TB/s, without alternatives 367 us.  What bounds it is the read of the logits (a plain read of them 330 to 375 us) and, at
 // the clock of 2.1 GHz that it gets, the vector unit: 7.5 instructions an entry, 10 with what the alternatives take, busy
 // all the time; without the entropy's two of them it takes 377 us where it took 416.
 // The alternatives ride on the softmax's own maxima: the `top`-th largest of the threads' largest entries is a lower bound of the
@@ -717,7 +717,8 @@ static int grad_pieces(int64_t T, int32_t V, int32_t dtype) {
 // Whether an array of T x V is read (or written) past the caches: it is beyond the last-level cache of 256 MiB, so it has left
 // before anybody can find it there.  us, kept / past, bf16, V = 151,936: logp with 20 alternatives 600 rows 54.1 / 52.8 (kept, for the
 // gradient that reads the same logits), 1,300 rows 95 / 91, 8,192 rows 441 / 412; gradient 900 rows 115 / 116, 1,300 rows
-// 168 / 164, 2,000 rows 250 / 256, 8,192 rows 1006 / 962.
+// 168 / 164, 2,000 rows 250 / 256, 8,192 rows 1006 / 962; from fp32 to bf16 600 rows 112 / 114, 1,300 rows 240 / 229, 4,000 rows 713 / 689; to fp32
+// from bf16 900 rows 194 / 188, 4,000 rows 813 / 792, from fp32 2,000 rows 501 / 518, 4,000 rows 954 / 930.
 static bool past_caches(int64_t T, int32_t V, int32_t dtype) {
   return T * V * (dtype == ADWIN_DT_BF16 ? 2 : 4) > ((int64_t)320 << 20);
 }
