@@ -500,10 +500,12 @@ def adwin_opd_quant_rows(x, row_status=False, q=None, scale=None) -> dict:
     N, H = x.shape
     if q is None:
         q = torch.empty(N, ADWIN_QUANT_PITCH(H), dtype=torch.int8, device=x.device)
+    else:
+        _flat("q", q, torch.int8, N, ADWIN_QUANT_PITCH(H))
     if scale is None:
         scale = torch.empty(N, dtype=torch.float32, device=x.device)
-    _flat("q", q, torch.int8, N, ADWIN_QUANT_PITCH(H))
-    _flat("scale", scale, torch.float32, N)
+    else:
+        _flat("scale", scale, torch.float32, N)
     out = {"q": q, "scale": scale}
     if row_status is True:
         out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
