@@ -507,11 +507,11 @@ def adwin_opd_quant_rows(x, row_status=False, q=None, scale=None) -> dict:
     else:
         _flat("scale", scale, torch.float32, N)
     out = {"q": q, "scale": scale}
-    if row_status is True:
-        out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
-    elif isinstance(row_status, torch.Tensor):
+    if isinstance(row_status, torch.Tensor):
         _flat("row_status", row_status, torch.int32, N)
         out["row_status"] = row_status
+    elif row_status:
+        out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
     p = adwin_opd_quant_problem(C.sizeof(adwin_opd_quant_problem), N, ld, H, _DTYPE[x.dtype], x.data_ptr(), q.data_ptr(),
                                 scale.data_ptr(), _ptr(out.get("row_status")))
     _check(lib.adwin_opd_quant_rows(p, _stream_handle(None)))

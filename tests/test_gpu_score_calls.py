@@ -65,6 +65,7 @@ def test_a_head_reports_what_it_could_not_compute(B):
     head = B.QuantHead(W.cuda())
     assert torch.equal(head.row_status.cpu(), (torch.arange(70) == 13).int() * B.ADWIN_DEV_NONFINITE)
     at = head.row_status.data_ptr()
+    assert torch.equal(B.adwin_opd_quant_rows(W.cuda(), row_status=1)["row_status"], head.row_status)
     z, status = head.logits(h.cuda(), row_status=True)
     assert torch.equal(z, head.logits(h.cuda())) and torch.all(z[4] == 0) and torch.all(z[:, 13] == 0)
     assert torch.equal(status.cpu(), (torch.arange(9) == 4).int() * B.ADWIN_DEV_NONFINITE)
