@@ -603,7 +603,8 @@ int adwin_opd_block_product(const adwin_opd_block_product_problem* p, void* work
  * may go where the old ones are.
  * A score of -inf: no candidates (a beam that is not there; its logits are not read).  Masked logits (-inf) are no candidates.  A row with
  * a NaN or +inf or of nothing but -inf, or a score of NaN or +inf, is excluded: no candidates, ADWIN_DEV_NONFINITE.
- * Ranks are computed in fp64 from sums of fp32 exponentials held in fp64.
+ * Ranks are computed in fp64 from sums of fp32 exponentials held in fp64, in an order that follows from the sizes alone: in one call the
+ * same logits give the same bits wherever their rows begin, so that beams of equal logits and scores have equal ranks.
  * Limits: 0 <= B, B K < 2^24, 1 <= K, keep <= ADWIN_MAX_BEAMS, 1 <= V <= 2^28, 0 <= length_power <= 8. */
 typedef struct adwin_opd_beam_select_problem {
   size_t  struct_bytes;

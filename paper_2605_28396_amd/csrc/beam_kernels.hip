@@ -35,6 +35,33 @@ __device__ __forceinline__ double rounded(double x, double y) {
   return p;
 }
 
+// A row in vectors from its first entry on, and up to a vector's entries behind them.  Which entries are added to one another follows from
+// their indices alone, never from where the row begins: beams of the same logits have the same log s, to the last bit, and rank by rising
+// beam.  A vector may begin at any address that suits its entries.  Against vectors from the first multiple of 16 bytes on, whose sums went by
+// the address, us: rows at multiples of 4 bytes the same (1,536 x 151,934 bf16 91 / 91, 768 x 151,935 fp32 85 / 85); bf16 rows at odd entries
+// 54 / 52 where the caches hold them (768 x 151,935), 108 / 90 where they do not (1,536 rows).
+template <typename T> struct Loose;
+template <> struct Loose<uint16_t> { typedef u32x4 Vec __attribute__((aligned(2))); };
+template <> struct Loose<float> { typedef u32x4 Vec __attribute__((aligned(4))); };
+template <typename T>
+struct BeamRow {
+  static constexpr int kPer = Entry<T>::kPerVec;
+  const T* p;
+  int vecs, edge;
+  __device__ __forceinline__ BeamRow(const T* row, int entries) : p(row), vecs(entries / kPer), edge(entries % kPer) {}
+  __device__ __forceinline__ int edge_index(int e) const { return vecs * kPer + e; }
+  template <bool PAST = false>
+  __device__ __forceinline__ uint4 vec(int i) const {
+    const typename Loose<T>::Vec* q = (const typename Loose<T>::Vec*)(p + (int64_t)i * kPer);
+    u32x4 v;
+    if constexpr (PAST) v = __builtin_nontemporal_load(q);
+    else v = *q;
+    return make_uint4(v[0], v[1], v[2], v[3]);
+  }
+  __device__ __forceinline__ int index(int i) const { return i * kPer; }
+};
+template <typename T> using BeamSpan = Piece<T, BeamRow<T>>;
+
 struct BeamSums { float r, m; double s; };
 constexpr float kFarRef = -16777216.f;     // the least reference: whole numbers next to some z c are good to a half up to here
 constexpr float kLeast = 1e-22f;            // the least c whose second part is a normal number
@@ -69,7 +96,7 @@ __device__ __forceinline__ float beam_add(BeamSums& a, const float (&x)[N], floa
 // The workgroup's sum, relative to e^base.  Where references do not hold (logits or 1 / temperature of millions, rows at a
 // mask's finite value), or c has no second part (its digits there would lie below 2^-126), the piece is read again, differences first.
 template <typename T>
-__device__ __forceinline__ BeamPart beam_piece(const Piece<T>& p, BeamSums a, const BeamArgs& g, float (*top)[2], double* sums) {
+__device__ __forceinline__ BeamPart beam_piece(const BeamSpan<T>& p, BeamSums a, const BeamArgs& g, float (*top)[2], double* sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float r = wave_max(a.r), m = wave_max(a.m);
   if (lane == 0) { top[wave][0] = r; top[wave][1] = m; }
@@ -115,7 +142,7 @@ __global__ __launch_bounds__(kThreads, 6) void beam_rows_kernel(BeamArgs a) {
   const int64_t row = blockIdx.x / (uint32_t)a.pieces;
   const int piece = (int)(blockIdx.x - (uint32_t)row * (uint32_t)a.pieces);
   if (!goes_on(a, row)) return;                      // the join sees that by itself
-  const Piece<T> p((const T*)a.z + row * a.ld, a.V, piece, a.pieces);
+  const BeamSpan<T> p((const T*)a.z + row * a.ld, a.V, piece, a.pieces);
   const int last = p.v1 - tid;                       // a thread's vectors: p.v0 + tid + 256 k below p.v1
   // whole steps, whose loads stand in no branch: the wait for a vector then leaves the younger ones in flight
   const int whole = (p.v1 - p.v0) / (kBeamStep * kThreads);

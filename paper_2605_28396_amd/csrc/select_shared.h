@@ -30,9 +30,9 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
 }
 
 // Part of a row: vectors [v0, v1), and the row's edge entries with the first part.
-template <typename T>
+template <typename T, typename Row = RowSpan<T>>
 struct Piece {
-  RowSpan<T> row;
+  Row row;
   int v0, v1, edge;
   __device__ __forceinline__ Piece(const T* p, int n, int piece, int pieces) : row(p, n) {
     v0 = (int)((int64_t)row.vecs * piece / pieces);
@@ -124,8 +124,8 @@ __device__ __forceinline__ void rank_keys(Select& l, const uint64_t* keys, int n
 // rising order).  Round by round over 256 vectors: a thread's largest key is ranked among the threads', the
 // top-th of these is a bound that at most `top` threads pass, and what passes it and the last of the kept ones is ranked
 // together with those.
-template <typename T>
-__device__ __forceinline__ void select_slowly(const Piece<T>& p, int top, Select& l) {
+template <typename T, typename Row>
+__device__ __forceinline__ void select_slowly(const Piece<T, Row>& p, int top, Select& l) {
   constexpr int N = Entry<T>::kPerVec;
   const int tid = threadIdx.x;
   int have = 0;
