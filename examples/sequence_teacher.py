@@ -83,7 +83,7 @@ class Student:
         out = B.adwin_opd_token_logp(z, ids)
         g = (-1.0 / scored).expand(n * steps).contiguous()
         dz = B.adwin_opd_token_logp_grad(z, ids, out["norm"], g)["dz"]
-        return -out["logp"].sum() / scored, h, self.head.grad(dz, h.detach(), dh_dtype=B.ADWIN_DT_F32)
+        return -out["logp"].sum() / scored, h, self.head.grad(dz, h.detach(), dh_dtype=B.ADWIN_DT_F32, status=status)
 
     def train_step(self, first, targets, length, lr):
         loss, h, grad = self.gradients(first, targets, length)

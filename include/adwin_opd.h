@@ -543,6 +543,8 @@ int adwin_opd_token_logp_grad(const adwin_opd_logp_grad_problem* p, void* hip_st
  * tile = 1 not.  What is given is written, zeros behind the last entry and the last scale of every row among it.
  * (Where that would stand for 2^128, beyond fp32, it is the largest that does not.)
  * An inf or NaN counts as 0 and sets ADWIN_DEV_NONFINITE in its row's word of row_status.
+ * x_status: a row whose word is not 0 is excluded: zeros, whatever it holds, and its word is that of row_status (which may not overlap
+ * it, ADWIN_E_ALIGN).
  * Limits: 0 <= N < 2^24 (and <= ADWIN_BLOCK_MAX_K across), 1 <= H <= ADWIN_BLOCK_MAX_K, fewer than 2^24 tiles of 128 x 128. */
 typedef struct adwin_opd_block_rows_problem {
   size_t  struct_bytes;      /* sizeof(adwin_opd_block_rows_problem), checked                  */
@@ -557,6 +559,7 @@ typedef struct adwin_opd_block_rows_problem {
   uint8_t* q_t;
   uint8_t* scale_t;
   int32_t* row_status;       /* [N], NULL = not wanted                                         */
+  const int32_t* x_status;   /* device [N], NULL = no row is excluded                          */
 } adwin_opd_block_rows_problem;
 int adwin_opd_block_rows(const adwin_opd_block_rows_problem* p, void* hip_stream);
 

@@ -126,7 +126,7 @@ class adwin_opd_block_rows_problem(C.Structure):
     _fields_ = [
         ("struct_bytes", C.c_size_t), ("N", C.c_int64), ("ld_x", C.c_int64), ("H", C.c_int32), ("x_dtype", C.c_int32),
         ("f8", C.c_int32), ("tile", C.c_int32), ("x", C.c_void_p), ("q", C.c_void_p), ("scale", C.c_void_p), ("q_t", C.c_void_p),
-        ("scale_t", C.c_void_p), ("row_status", C.c_void_p),
+        ("scale_t", C.c_void_p), ("row_status", C.c_void_p), ("x_status", C.c_void_p),
     ]
 
 
@@ -738,19 +738,20 @@ def _made(name, t, dtype, shape, device):
 
 @_on_stream
 def adwin_opd_block_rows(x, tile=1, f8=ADWIN_F8_E4M3, along=True, across=False, row_status=False, q=None, scale=None, q_t=None,
-                         scale_t=None) -> dict:
+                         scale_t=None, x_status=None) -> dict:
     """Rows x [N, H] (bf16, fp32) as 8-bit floats with a power-of-two scale (its exponent's byte) for each block of 128 entries
     of a row, or of 128 rows with tile = 128.  along: `q` [N, ADWIN_BLOCK_PITCH(H)], `scale` [ceil(N / tile),
     ADWIN_BLOCK_SCALES(H)]; across: blocks of x transposed, `q_t` [H, ADWIN_BLOCK_PITCH(N)], `scale_t`, for products that
-    contract over the rows.  `row_status` [N] if wanted.  q, scale, q_t, scale_t, row_status: where they go; else new
-    tensors."""
+    contract over the rows.  `row_status` [N] if wanted.  x_status [N]: rows whose word is not 0 are excluded, zeros.
+    q, scale, q_t, scale_t, row_status: where they go; else new tensors."""
     ld = _rows("x", x)
-    _here(x, q, scale, q_t, scale_t, row_status if isinstance(row_status, torch.Tensor) else None)
+    _here(x, q, scale, q_t, scale_t, row_status if isinstance(row_status, torch.Tensor) else None, x_status)
     N, H = x.shape
     if f8 not in (ADWIN_F8_E4M3, ADWIN_F8_E5M2) or tile not in (1, 128):
         raise AdwinError(ADWIN_E_MODE)
     if H > ADWIN_BLOCK_MAX_K:                          # 32 bits do not hold any
         raise AdwinError(ADWIN_E_SHAPE)
+    s_ptr = _flat("x_status", x_status, torch.int32, N) if x_status is not None else None
     dt, out = _TORCH_F8[f8], {}
     if along:
         out["q"] = _made("q", q, dt, (N, ADWIN_BLOCK_PITCH(H)), x.device)
@@ -765,7 +766,7 @@ def adwin_opd_block_rows(x, tile=1, f8=ADWIN_F8_E4M3, along=True, across=False, 
         out["row_status"] = torch.empty(N, dtype=torch.int32, device=x.device)
     p = adwin_opd_block_rows_problem(C.sizeof(adwin_opd_block_rows_problem), N, ld, H, _DTYPE[x.dtype], f8, tile, x.data_ptr(),
                                      _ptr(out.get("q")), _ptr(out.get("scale")), _ptr(out.get("q_t")), _ptr(out.get("scale_t")),
-                                     _ptr(out.get("row_status")))
+                                     _ptr(out.get("row_status")), s_ptr)
     _check(lib.adwin_opd_block_rows(p, _stream_handle(None)))
     return out
 
@@ -862,9 +863,14 @@ class BlockHead:
         return (z, x["row_status"]) if row_status else z
 
     @_on_stream
-    def grad(self, dz, h=None, f8=ADWIN_F8_E4M3, dh_dtype=ADWIN_DT_BF16, dW_dtype=ADWIN_DT_F32, dh=None, dW=None, want_dh=True) -> dict:
+    def grad(self, dz, h=None, f8=ADWIN_F8_E4M3, dh_dtype=ADWIN_DT_BF16, dW_dtype=ADWIN_DT_F32, dh=None, dW=None, want_dh=True, status=None,
+             row_status=False) -> dict:
         """The gradients of a loss by hidden states and weights, of its derivatives dz [T, V] by the logits: `dh` [T, H] = dz W, and
-        with h also `dW` [V, H] = dz^T h, both from dz in blocks of 8-bit floats of format f8.  An inf or NaN in dz or h counts as 0."""
+        with h also `dW` [V, H] = dz^T h, both from dz in blocks of 8-bit floats of format f8.
+
+        status [T], as logits() gives it: a row whose word is not 0 has logits that depend on nothing, and so no gradient: 0 in dh, no part of
+        dW, whatever dz and h hold there.  In other rows an inf or NaN in dz or h counts as 0; with row_status `dz_status` and, with h,
+        `h_status` [T] say in which: ADWIN_DEV_NONFINITE, or the word of `status`."""
         if dz.dim() != 2 or dz.shape[1] != self.V or (h is not None and tuple(h.shape) != (dz.shape[0], self.H)):
             raise ValueError(f"dz: [T, {self.V}] and h: [T, {self.H}] are taken, not {tuple(dz.shape)}"
                              + ("" if h is None else f" and {tuple(h.shape)}"))
@@ -873,10 +879,16 @@ class BlockHead:
         out = {}
         if not want_dh and h is None:
             return out
-        d = adwin_opd_block_rows(dz, f8=f8, along=want_dh, across=h is not None)
+        row_status = bool(row_status)
+        d = adwin_opd_block_rows(dz, f8=f8, along=want_dh, across=h is not None, row_status=row_status, x_status=status)
+        if row_status:
+            out["dz_status"] = d["row_status"]
         if want_dh:
             out["dh"] = adwin_opd_block_product(d["q"], d["scale"], self.W_q_t, self.W_scale_t, b_tile=128, c_dtype=dh_dtype, c=dh)["c"]
         if h is not None:
+            t = adwin_opd_block_rows(h, along=False, across=True, row_status=row_status, x_status=status)
+            if row_status:
+                out["h_status"] = t["row_status"]
             if dz.shape[0] == 0:
                 if dW is None:
                     dW = torch.empty(self.V, self.H, dtype=_TORCH_DTYPE[dW_dtype], device=dz.device)
@@ -884,7 +896,6 @@ class BlockHead:
                     raise ValueError(f"dW: {(self.V, self.H)} is taken, not {tuple(dW.shape)}")
                 out["dW"] = dW.zero_()
                 return out
-            t = adwin_opd_block_rows(h, along=False, across=True)
             out["dW"] = adwin_opd_block_product(d["q_t"], d["scale_t"], t["q_t"], t["scale_t"], c_dtype=dW_dtype, c=dW)["c"]
         return out
 

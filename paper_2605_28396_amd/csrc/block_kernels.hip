@@ -20,7 +20,7 @@ struct BlockRowsArgs {
   int32_t H, tile;
   int32_t along, across;
   uint8_t* q; uint8_t* scale; uint8_t* q_t; uint8_t* scale_t;
-  int32_t* row_status;
+  int32_t* row_status; const int32_t* x_status;
   int64_t pitch, scales, pitch_t, scales_t;       // bytes from row to row
 };
 
@@ -69,9 +69,10 @@ __device__ __forceinline__ void keep_within(Eight<T>& v) {
     v.v[i >> 2][i & 3] = w;
   }
 }
-__global__ __launch_bounds__(256) void clear_status_kernel(int32_t* status, int64_t n) {
+// words of excluded rows, else zeros
+__global__ __launch_bounds__(256) void begin_status_kernel(int32_t* status, const int32_t* excluded, int64_t n) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) status[i] = 0;
+  if (i < n) status[i] = excluded ? excluded[i] : 0;
 }
 
 // The largest of the 16 lanes of a block, in all of them, by rotations within them, which take no turn of the LDS.
@@ -98,6 +99,7 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockRowsArgs p) {
   const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (n >= p.N) return;
   const T* x = (const T*)p.x + n * p.ld;
+  const int H = p.x_status && p.x_status[n] != 0 ? 0 : p.H;      // entries that are read
   const int c0 = (int)blockIdx.y * (512 * kUnits) + 8 * lane;
   Eight<T> v[kUnits];
 #pragma unroll
@@ -105,9 +107,9 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockRowsArgs p) {
     const int c = c0 + 512 * u;
     v[u].clear();
     if constexpr (WHOLE) {
-      if (c < p.H) v[u].template load<PAST>(x + c);
-    } else if (c < p.H) {
-      v[u].load_some(x + c, p.H - c);
+      if (c < H) v[u].template load<PAST>(x + c);
+    } else if (c < H) {
+      v[u].load_some(x + c, H - c);
     }
   }
   bool bad = false;
@@ -141,13 +143,21 @@ __global__ __launch_bounds__(256) void block_tile_kernel(BlockRowsArgs p) {
   const uint32_t tiles = (uint32_t)(p.pitch / 128), down = blockIdx.x / tiles, right = blockIdx.x - down * tiles;
   const int64_t n0 = (int64_t)down * 128;
   const int c0 = (int)right * 128, c = c0 + 8 * l;
+  uint32_t excluded = 0;                               // bits of the thread's rows
+  if (p.x_status) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int64_t n = n0 + 8 * g + r;
+      if (n < p.N && p.x_status[n] != 0) excluded |= 1u << r;
+    }
+  }
   Eight<T> v[8];
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     const int64_t n = n0 + 8 * g + r;
     const T* x = (const T*)p.x + n * p.ld + c;
     v[r].clear();
-    if (n < p.N && c < p.H) {
+    if (n < p.N && c < p.H && !(excluded >> r & 1)) {
       if constexpr (WHOLE) v[r].template load<PAST>(x);
       else v[r].load_some(x, p.H - c);
     }
@@ -1343,11 +1353,13 @@ extern "C" int adwin_opd_block_rows(const adwin_opd_block_rows_problem* p, void*
   if (!p->x || !p->q != !p->scale || !p->q_t != !p->scale_t || (!p->q && !p->q_t)) return ADWIN_E_NULL;
   if (((uintptr_t)p->x & entry_mask(p->x_dtype)) || (((uintptr_t)p->q | (uintptr_t)p->q_t | (uintptr_t)p->scale | (uintptr_t)p->scale_t) & 15))
     return ADWIN_E_ALIGN;
+  // words of row_status are set while others are still asked for whether their row is excluded
+  if (p->row_status && p->x_status && p->row_status < p->x_status + p->N && p->x_status < p->row_status + p->N) return ADWIN_E_ALIGN;
   hipStream_t stream = (hipStream_t)hip_stream;
   BlockRowsArgs a{};
   a.x = p->x; a.ld = p->ld_x; a.N = p->N; a.H = p->H; a.tile = p->tile;
   a.along = p->q != nullptr; a.across = p->q_t != nullptr;
-  a.q = p->q; a.scale = p->scale; a.q_t = p->q_t; a.scale_t = p->scale_t; a.row_status = p->row_status;
+  a.q = p->q; a.scale = p->scale; a.q_t = p->q_t; a.scale_t = p->scale_t; a.row_status = p->row_status; a.x_status = p->x_status;
   a.pitch = ADWIN_BLOCK_PITCH((int64_t)p->H); a.scales = ADWIN_BLOCK_SCALES((int64_t)p->H);
   a.pitch_t = ADWIN_BLOCK_PITCH(p->N); a.scales_t = ADWIN_BLOCK_SCALES(p->N);
   const int64_t size = p->x_dtype == ADWIN_DT_BF16 ? 2 : 4;
@@ -1356,7 +1368,7 @@ extern "C" int adwin_opd_block_rows(const adwin_opd_block_rows_problem* p, void*
   // 461 / 481 (along alone 318 / 344); fp32, whose eight entries are two loads, 188 / 183
   const bool past = whole && size == 2 && a.N * a.H * size > ((int64_t)96 << 20);
   if (a.row_status) {
-    clear_status_kernel<<<(unsigned)((a.N + 255) / 256), 256, 0, stream>>>(a.row_status, a.N);
+    begin_status_kernel<<<(unsigned)((a.N + 255) / 256), 256, 0, stream>>>(a.row_status, a.x_status, a.N);
     ADWIN_HIP_TRY(hipGetLastError());
   }
 #define ADWIN_LAUNCH_T(KERNEL, GRID, T, F8)                                     \
