@@ -1416,7 +1416,7 @@ extern "C" int adwin_opd_block_product(const adwin_opd_block_product_problem* p,
   const BlockWay way(p);
   if (way.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < way.bytes)) return ADWIN_E_WORKSPACE;
   hipStream_t stream = (hipStream_t)hip_stream;
-  if (first_use_on_device(3)) ADWIN_HIP_TRY(block_kernels_opt_in());
+  ADWIN_HIP_TRY(once_on_device(kOnceBlocks, block_kernels_opt_in));
   BlockArgs a{};
   a.a = p->a; a.a_scale = p->a_scale; a.b = p->b; a.b_scale = p->b_scale; a.a_status = p->a_status;
   a.M = p->M; a.N = (int32_t)p->N; a.pitch = ADWIN_BLOCK_PITCH(p->K); a.scales = ADWIN_BLOCK_SCALES(p->K);

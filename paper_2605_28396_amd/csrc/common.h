@@ -21,10 +21,10 @@ struct DevicePlan {
   int32_t* row_seq;          // [n_pad] rollout of each computed row
 };
 
-// True the first time it is called for (slot, current device): function attributes such as
-// the dynamic-LDS opt-in are per device, so they are set once on every device that is used.
-// `slot` distinguishes call sites (0..3).  Thread-safe.
-bool first_use_on_device(int slot);
+// Runs `prepare` unless it has succeeded on the current device before: function attributes such as the dynamic-LDS
+// opt-in are per device, so they are set once on every device that is used, before any launch there.  Thread-safe.
+enum Once { kOnceSweeps, kOnceLogits, kOnceQuant, kOnceBlocks, kOnce };
+hipError_t once_on_device(Once what, hipError_t (*prepare)());
 
 void set_last_hip_error(hipError_t e, const char* where);
 

@@ -380,28 +380,25 @@ static int check_problem(const adwin_opd_problem* p) {
   return ADWIN_OK;
 }
 
-static hipError_t ensure_lds_opt_in() {
-  if (!first_use_on_device(0)) return hipSuccess;
+static hipError_t lds_opt_in() {
   hipError_t e = sweep_kernels_opt_in();
   if (e != hipSuccess) return e;
   return grad_kernels_opt_in();
 }
+static hipError_t ensure_lds_opt_in() { return once_on_device(kOnceSweeps, lds_opt_in); }
 
 }  // namespace adwin
 
 using namespace adwin;
 
 extern "C" int adwin_opd_init(void) {
-  ADWIN_HIP_TRY(sweep_kernels_opt_in());
-  ADWIN_HIP_TRY(grad_kernels_opt_in());
+  ADWIN_HIP_TRY(lds_opt_in());
   ADWIN_HIP_TRY(logits_kernels_opt_in());
   ADWIN_HIP_TRY(logits_static_setup());
   ADWIN_HIP_TRY(quant_kernels_opt_in());
   ADWIN_HIP_TRY(block_kernels_opt_in());
-  (void)first_use_on_device(0);      // the calls need not repeat it on this device
-  (void)first_use_on_device(1);
-  (void)first_use_on_device(2);
-  (void)first_use_on_device(3);
+  for (int what = 0; what < kOnce; ++what)      // the calls need not repeat it on this device
+    ADWIN_HIP_TRY(once_on_device((Once)what, [] { return hipSuccess; }));
   return ADWIN_OK;
 }
 

@@ -1,9 +1,9 @@
 // The little state the library keeps: per device, whether the kernel attributes have been set;
 // per thread, the text of the last HIP error.
-#include <atomic>
 #include <cstdio>
 
 #include "common.h"
+#include "device_once.h"
 
 namespace adwin {
 
@@ -16,12 +16,11 @@ void set_last_hip_error(hipError_t e, const char* where) {
            hipGetErrorString(e), where);
 }
 
-bool first_use_on_device(int slot) {
-  static std::atomic<unsigned long long> seen[4];
+hipError_t once_on_device(Once what, hipError_t (*prepare)()) {
+  static DeviceOnce once[kOnce];
   int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev > 63 || slot < 0 || slot > 3) return true;
-  const unsigned long long bit = 1ull << dev;
-  return (seen[slot].fetch_or(bit) & bit) == 0;
+  if (hipGetDevice(&dev) != hipSuccess) dev = -1;
+  return once[what].run(dev, prepare);
 }
 
 }  // namespace adwin

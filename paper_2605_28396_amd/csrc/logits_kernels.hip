@@ -1087,7 +1087,7 @@ static int logits_impl(const adwin_opd_logits_problem* p, void* workspace, size_
       if (diag) logits_row_kernel<true><<<(unsigned)p->T, kRowThreads, 0, stream>>>(a);
       else logits_row_kernel<false><<<(unsigned)p->T, kRowThreads, 0, stream>>>(a);
     } else {
-      if (first_use_on_device(1)) ADWIN_HIP_TRY(logits_kernels_opt_in());
+      ADWIN_HIP_TRY(once_on_device(kOnceLogits, logits_kernels_opt_in));
 #define ADWIN_LAUNCH(...) logits_row_resident_kernel<__VA_ARGS__><<<(unsigned)p->T, kResThreads, kResLdsBytes, stream>>>(a)
       if (diag && past) ADWIN_LAUNCH(true, true);
       else if (diag) ADWIN_LAUNCH(true, false);

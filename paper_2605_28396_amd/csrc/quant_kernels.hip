@@ -879,7 +879,7 @@ hipError_t quant_kernels_opt_in() {
   }
   return hipSuccess;
 }
-static hipError_t quant_opt_in() { return first_use_on_device(2) ? quant_kernels_opt_in() : hipSuccess; }
+static hipError_t quant_opt_in() { return once_on_device(kOnceQuant, quant_kernels_opt_in); }
 
 static hipError_t launch_quant_rows(const QuantArgs& a, int32_t dtype, hipStream_t st) {
   const int64_t blocks = (a.N + 3) / 4;
