@@ -647,7 +647,7 @@ typedef struct adwin_opd_beam_state {
   int32_t planes, reserved;  /* 0                                                              */
 } adwin_opd_beam_state;
 /* Limits: 0 <= B, B K < 2^24, B keep < 2^24, 1 <= K, keep <= ADWIN_MAX_BEAMS, 0 <= n <= ADWIN_MAX_STATES, planes < 2^20,
- * positions bytes < 2^40, pitches that keep planes and rows apart. */
+ * positions bytes < 2^40, pitches below 2^40 that keep planes and rows apart, and less than 2^48 bytes from an array's first to its last. */
 typedef struct adwin_opd_beam_reorder_problem {
   size_t  struct_bytes;
   int64_t B;

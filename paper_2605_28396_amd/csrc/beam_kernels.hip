@@ -572,6 +572,11 @@ static int check_reorder(const adwin_opd_beam_reorder_problem* p) {
     if (s.from_plane < 0 || s.to_plane < 0 || s.from_plane >= most || s.to_plane >= most || s.from_row < 0 || s.to_row < 0 ||
         s.from_row >= most || s.to_row >= most)
       return ADWIN_E_SHAPE;
+    // from an array's first byte to its last: within the addresses of a device, so that what follows stays within 64 bits
+    auto ends = [&](int64_t row, int64_t pl, int64_t rows) {
+      return (__int128)(rows - 1) * row + (__int128)(s.planes - 1) * pl + plane < (__int128)1 << 48;
+    };
+    if (!ends(s.from_row, s.from_plane, p->B * p->K) || !ends(s.to_row, s.to_plane, p->B * p->keep)) return ADWIN_E_SHAPE;
     // planes inside a row, or rows inside a plane: either way they must be apart
     auto apart = [&](int64_t row, int64_t pl, int64_t rows) {
       if (s.planes > 1 && pl < plane) return false;

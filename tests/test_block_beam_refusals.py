@@ -20,3 +20,27 @@ def test_words_of_excluded_rows_are_not_those_written(B):
         assert B.lib.adwin_opd_block_rows(C.byref(p), None) == B.ADWIN_E_ALIGN, at
     p = _struct(B.adwin_opd_block_rows_problem, base, dict(N=0, x_status=PTR + 4096))
     assert B.lib.adwin_opd_block_rows(C.byref(p), None) == B.ADWIN_OK
+
+
+def _reorder(B, n, K, **state):
+    """The status of a move of `n` sequences of K beams, one array at PTR to 2^45 bytes behind it."""
+    s = (B.adwin_opd_beam_state * 1)()
+    for k, v in {**{"from": PTR, "to": PTR + (1 << 45), "positions": 16, "bytes": 4, "planes": 1}, **state}.items():
+        setattr(s[0], k, v)
+    p = B.adwin_opd_beam_reorder_problem(C.sizeof(B.adwin_opd_beam_reorder_problem), n, K, K, 1, 0, C.addressof(s), PTR - 64, None)
+    return B.lib.adwin_opd_beam_reorder(C.byref(p), None)
+
+
+def test_moves_of_rows_beyond_any_address_are_refused(B):
+    """Distances of rows whose sum leaves 64 bits: such planes and rows count as apart, and such arrays as without end, if it is not looked at."""
+    far, n = (1 << 40) - 16, (1 << 18) - 1                           # 2^24 - 64 rows: (rows - 1) far is 2^64 and little less
+    assert _reorder(B, n, 64, from_row=far, to_row=far) == B.ADWIN_E_SHAPE
+    assert _reorder(B, n, 64, from_row=64, to_row=far) == _reorder(B, n, 64, from_row=far, to_row=64) == B.ADWIN_E_SHAPE
+    # the rows of one plane lie over the other planes
+    assert _reorder(B, n, 64, from_row=far, to_row=far, planes=10, from_plane=1 << 39, to_plane=1 << 39) == B.ADWIN_E_SHAPE
+    assert _reorder(B, 1 << 17, 64, from_row=far, to_row=far) == B.ADWIN_E_SHAPE              # 2^63 and little less
+    planes = (1 << 20) - 1
+    assert _reorder(B, 1, 1, planes=planes, from_plane=far, to_plane=far) == B.ADWIN_E_SHAPE
+    # 2^48 bytes from the first to the last, and 16 fewer: only these get as far as a move in place that is none
+    edge = dict(to=PTR, planes=257, from_plane=far, to_plane=far - 16)
+    assert _reorder(B, 1, 1, positions=1024, **edge) == B.ADWIN_E_SHAPE and _reorder(B, 1, 1, positions=1020, **edge) == B.ADWIN_E_ALIGN
