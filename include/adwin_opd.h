@@ -603,7 +603,7 @@ int adwin_opd_block_product(const adwin_opd_block_product_problem* p, void* work
  * total / max(1, length)^length_power, length one more than the beam's where it goes on; equal ones by rising beam and then, within
  * a beam, by falling logit and rising token.  The `keep` best, in that order, give parent (k), token, score (the total), finished
  * (it was, or the token is `end`) and length; where there are fewer: -1, -1, -inf, 0, 0.  With keep = K the new score, finished and length
- * may go where the old ones are.
+ * may go where the old ones are; otherwise what a call writes may overlap nothing else that it reads or writes (ADWIN_E_ALIGN).
  * A score of -inf: no candidates (a beam that is not there; its logits are not read).  Masked logits (-inf) are no candidates.  A row with
  * a NaN or +inf or of nothing but -inf, or a score of NaN or +inf, is excluded: no candidates, ADWIN_DEV_NONFINITE.
  * Ranks are computed in fp64 from sums of fp32 exponentials held in fp64, in an order that follows from the sizes alone: in one call the

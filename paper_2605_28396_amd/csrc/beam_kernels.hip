@@ -540,6 +540,27 @@ static int check_select(const adwin_opd_beam_select_problem* p) {
   return ADWIN_OK;
 }
 
+// What a call writes may overlap nothing else that it reads or writes: other sequences may still be read.  With keep = K new scores, ends and
+// lengths may go where the old ones are, as a sequence's are read before its own are written.
+static bool selects_apart(const adwin_opd_beam_select_problem* p, const void* workspace, size_t workspace_bytes) {
+  const int64_t beams = 4 * p->B * p->K, kept = 4 * p->B * p->keep, size = p->z_dtype == ADWIN_DT_BF16 ? 2 : 4;
+  struct Array { const void* at; int64_t bytes; const void* in_place; };
+  const Array written[] = {{p->parent, kept, nullptr}, {p->token, kept, nullptr}, {p->new_score, kept, p->score}, {p->new_finished, kept, p->finished},
+                           {p->new_length, kept, p->length}, {p->row_status, beams, nullptr}, {workspace, (int64_t)workspace_bytes, nullptr}};
+  const Array read[] = {{p->z, ((p->B * p->K - 1) * p->ld_z + p->V) * size, nullptr}, {p->score, beams, nullptr}, {p->finished, beams, nullptr},
+                        {p->length, beams, nullptr}};
+  auto meet = [](const Array& a, const Array& b) {
+    return a.at && b.at && (const char*)a.at < (const char*)b.at + b.bytes && (const char*)b.at < (const char*)a.at + a.bytes;
+  };
+  for (const Array& w : written) {
+    for (const Array& r : read)
+      if (meet(w, r) && !(p->keep == p->K && w.at == r.at && w.in_place == r.at)) return false;
+    for (const Array* o = written; o != &w; ++o)
+      if (meet(w, *o)) return false;
+  }
+  return true;
+}
+
 struct BeamLayout {
   int pieces;
   size_t o_keys, bytes;
@@ -663,6 +684,7 @@ extern "C" int adwin_opd_beam_select(const adwin_opd_beam_select_problem* p, voi
   if ((uintptr_t)p->z & entry_mask(p->z_dtype)) return ADWIN_E_ALIGN;
   const BeamLayout L(p);
   if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < L.bytes) return ADWIN_E_WORKSPACE;
+  if (!selects_apart(p, workspace, L.bytes)) return ADWIN_E_ALIGN;
   BeamArgs a{};
   a.z = p->z; a.ld = p->ld_z; a.B = p->B; a.rows = p->B * p->K; a.K = p->K; a.keep = p->keep; a.V = p->V; a.pieces = L.pieces;
   a.end = p->end < 0 ? -1 : p->end;

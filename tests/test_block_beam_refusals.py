@@ -44,3 +44,31 @@ def test_moves_of_rows_beyond_any_address_are_refused(B):
     # 2^48 bytes from the first to the last, and 16 fewer: only these get as far as a move in place that is none
     edge = dict(to=PTR, planes=257, from_plane=far, to_plane=far - 16)
     assert _reorder(B, 1, 1, positions=1024, **edge) == B.ADWIN_E_SHAPE and _reorder(B, 1, 1, positions=1020, **edge) == B.ADWIN_E_ALIGN
+
+
+def test_selections_over_what_they_read_are_refused(B):
+    """Other sequences may still be read: only with keep = K do new scores, ends and lengths go where the old ones are, exactly."""
+    names = ("z", "score", "finished", "length", "parent", "token", "new_score", "new_finished", "new_length", "row_status")
+    at = {n: PTR + (i + 1) * (1 << 20) for i, n in enumerate(names)}
+    base = dict(B=7, ld_z=1000, K=3, keep=3, V=1000, z_dtype=0, end=-1, temperature=1.0, length_power=0.0, **at)
+    ws = PTR + (1 << 30)
+
+    def st(workspace=ws, **over):
+        p = _struct(B.adwin_opd_beam_select_problem, base, over)
+        return B.lib.adwin_opd_beam_select(C.byref(p), workspace, 1 << 28, None)
+    need = B.adwin_opd_beam_select_workspace_bytes(_struct(B.adwin_opd_beam_select_problem, base, {}))
+    read, written = names[:4], names[4:]
+    old = {"new_" + n: n for n in ("score", "finished", "length")}
+    for w in written:
+        for r in names:
+            if r == w:
+                continue
+            for keep, offset in ((2, 0), (3, 4), (3, -4), (3, 0), (4, 0), (4, 80), (4, -108)):     # 84 bytes of beams, 112 of four kept
+                if (keep == 3 and offset == 0 and old.get(w) == r) or (keep == 4 and offset == -108 and w == "row_status"):
+                    continue
+                assert st(keep=keep, **{w: at[r] + offset}) == B.ADWIN_E_ALIGN, (w, r, keep, offset)
+    assert st(parent=at["z"] + 2 * (20 * 1000 + 1000) - 4) == B.ADWIN_E_ALIGN                      # the last logits
+    for name in names:
+        assert st(**{name: ws + need - 4}) == B.ADWIN_E_ALIGN, name
+    # the old ones' places, but another is in the way
+    assert st(new_score=at["score"], new_length=at["score"]) == st(new_score=at["finished"]) == B.ADWIN_E_ALIGN
