@@ -1247,14 +1247,16 @@ static int check_product(const adwin_opd_block_product_problem* p) {
 }
 
 // Groups of 16 tokens of the kernel for few tokens, 0 where tiles serve the call: fp32 results of up to 32 tokens as far as they fit the LDS,
-// where b comes from memory (it is beyond the last-level cache of 256 MiB) or the sums are short.  us, few / tiles, fp32, 1 token: V = 151,936,
-// K = 4096 113 / 133, K = 2048 53 / 62, V = 75,000, K = 4096 53 / 69; K = 1024, V = 4,000 6.9 / 8.6, V = 50,000 14.3 / 15.6; V = 16,000, K = 4096
-// 17.4 / 17.4, V = 30,000, K = 2048 17 / 15.  32 tokens: V = 151,936, K = 4096 133 / 133, K = 2048 65 / 69, V = 50,000, K = 1024 15.8 / 16.4.
+// where b is large or the sums are short.  us, few / tiles, fp32, 1 token: K = 4096, V = 16,000 17.5 / 17.1, 30,000 24.6 / 25.0,
+// 35,000 24.8 / 36, 45,000 31 / 39, 75,000 50 / 69, 151,936 113 / 133; K = 2048, V = 60,000 25.2 / 25.6, 80,000 30 / 36, 151,936 53 / 64;
+// K = 10,000, V = 14,000 30.4 / 30.1, 18,000 34 / 46; K = 1280, V = 100,000 24.5 / 31.3; K = 1024, V = 4,000 6.9 / 8.6, 50,000 14.3 / 15.6.  32 tokens:
+// K = 4096, V = 16,000 21 / 19, 30,000 28.5 / 24.3, 35,000 29 / 39, 45,000 35 / 42, 151,936 133 / 133; K = 2048, V = 60,000 27.3 / 26.5,
+// 80,000 32 / 37, 151,936 66 / 72.  16 tokens, K = 10,000, V = 14,000 33 / 31.
 static int few_tokens(const adwin_opd_block_product_problem* p) {
   const int64_t n = (p->M + 15) / 16;
   const int pitch = ADWIN_BLOCK_PITCH(p->K);
   if (p->c_dtype != ADWIN_DT_F32 || n < 1 || n > 2 || p->N < 1 || pitch > 16384 || few_lds((int)n, pitch) > 160 * 1024) return 0;
-  return p->N * pitch >= (int64_t)288 << 20 || pitch <= 1024 ? (int)n : 0;
+  return p->N * pitch >= (int64_t)128 << 20 || pitch <= 1024 ? (int)n : 0;
 }
 
 // How a product is served: by the kernel for few tokens (fn < 0), or by tiles of 64 fn tokens, its contraction in `splits` parts.

@@ -23,7 +23,8 @@ def B():
 
 # Entries of -1 to 1 and scales of 1 and 2, at random: products of 0 to 4, of which nothing is cut, and sums within 2^20, exact in fp32.
 LONG = [(1, 20, 65536), (5, 33, 9000), (40, 60, 30001), (100, 1000, 33333), (200, 2000, 30001), (700, 600, 50007), (600, 2050, 24000),
-        (2049, 4097, 40000), (3000, 3001, 33000), (512, 2048, 151936), (3, 40001, 8200), (17, 70001, 4500), (1, 30001, 10100), (1100, 300, 5000)]
+        (2049, 4097, 40000), (3000, 3001, 33000), (512, 2048, 151936), (3, 40001, 8200), (17, 70001, 4500), (1, 30001, 10100), (1100, 300, 5000),
+        (5, 30001, 4600), (32, 40003, 4100)]
 
 
 @pytest.mark.parametrize("M,N,K", LONG)
