@@ -1366,31 +1366,34 @@ extern "C" int adwin_opd_block_rows(const adwin_opd_block_rows_problem* p, void*
   a.pitch_t = ADWIN_BLOCK_PITCH(p->N); a.scales_t = ADWIN_BLOCK_SCALES(p->N);
   const int64_t size = p->x_dtype == ADWIN_DT_BF16 ? 2 : 4;
   const bool whole = ((uintptr_t)a.x & 15) == 0 && ((a.ld * size) & 15) == 0 && (a.H & 7) == 0;
-  // past the caches from 96 MiB of bf16 on.  us, past / kept: 30,000 x 4096 72 / 75, both ways 1,024 x 151,936 124 / 134, 151,936 x 4096 in tiles
-  // 461 / 481 (along alone 318 / 344); fp32, whose eight entries are two loads, 188 / 183
-  const bool past = whole && size == 2 && a.N * a.H * size > ((int64_t)96 << 20);
+  // past the caches from 96 MiB of bf16 on, and from 256 of fp32 along the rows.  us, past / kept: bf16 30,000 x 4096 72 / 75, both ways
+  // 1,024 x 151,936 124 / 134, 151,936 x 4096 in tiles 461 / 481 (along alone 318 / 344); fp32 along the rows 15,000 x 4096 58 / 50,
+  // 18,000 69 / 75, 30,000 114 / 132, 151,936 x 2048 269 / 289, both ways 30,000 x 4096 145 / 142, in tiles 137 / 141
+  const bool alone = a.tile == 1 && !a.across;
+  const bool past = whole && (size == 2 || alone) && a.N * a.H * size > ((int64_t)(size == 2 ? 96 : 256) << 20);
   if (a.row_status) {
     begin_status_kernel<<<(unsigned)((a.N + 255) / 256), 256, 0, stream>>>(a.row_status, a.x_status, a.N);
     ADWIN_HIP_TRY(hipGetLastError());
   }
-#define ADWIN_LAUNCH_T(KERNEL, GRID, T, F8)                                     \
-  if (past) KERNEL<T, F8, true, true><<<GRID, 256, 0, stream>>>(a);             \
+  // PAST: whether `past` occurs
+#define ADWIN_LAUNCH_T(KERNEL, GRID, T, F8, PAST)                               \
+  if (PAST && past) KERNEL<T, F8, true, PAST><<<GRID, 256, 0, stream>>>(a);     \
   else if (whole) KERNEL<T, F8, true, false><<<GRID, 256, 0, stream>>>(a);      \
   else KERNEL<T, F8, false, false><<<GRID, 256, 0, stream>>>(a);
-#define ADWIN_LAUNCH(KERNEL, GRID)                                              \
-  if (p->x_dtype == ADWIN_DT_BF16) {                                            \
-    if (p->f8 == ADWIN_F8_E4M3) { ADWIN_LAUNCH_T(KERNEL, GRID, uint16_t, 0) }   \
-    else { ADWIN_LAUNCH_T(KERNEL, GRID, uint16_t, 1) }                          \
-  } else {                                                                      \
-    if (p->f8 == ADWIN_F8_E4M3) { ADWIN_LAUNCH_T(KERNEL, GRID, float, 0) }      \
-    else { ADWIN_LAUNCH_T(KERNEL, GRID, float, 1) }                             \
+#define ADWIN_LAUNCH(KERNEL, GRID, PAST_F32)                                            \
+  if (p->x_dtype == ADWIN_DT_BF16) {                                                    \
+    if (p->f8 == ADWIN_F8_E4M3) { ADWIN_LAUNCH_T(KERNEL, GRID, uint16_t, 0, true) }     \
+    else { ADWIN_LAUNCH_T(KERNEL, GRID, uint16_t, 1, true) }                            \
+  } else {                                                                              \
+    if (p->f8 == ADWIN_F8_E4M3) { ADWIN_LAUNCH_T(KERNEL, GRID, float, 0, PAST_F32) }    \
+    else { ADWIN_LAUNCH_T(KERNEL, GRID, float, 1, PAST_F32) }                           \
   }
-  if (a.tile == 1 && !a.across) {
+  if (alone) {
     const dim3 grid((unsigned)((a.N + 3) / 4), (unsigned)((a.pitch + 512 * kUnits - 1) / (512 * kUnits)));
-    ADWIN_LAUNCH(block_rows_kernel, grid)
+    ADWIN_LAUNCH(block_rows_kernel, grid, true)
   } else {
     const dim3 grid((unsigned)(a.pitch / 128 * ((a.N + 127) / 128)));
-    ADWIN_LAUNCH(block_tile_kernel, grid)
+    ADWIN_LAUNCH(block_tile_kernel, grid, false)
   }
 #undef ADWIN_LAUNCH
 #undef ADWIN_LAUNCH_T

@@ -113,9 +113,10 @@ def test_sums_are_not_cut(B, M, N):
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
-@pytest.mark.parametrize("dtype,N,H", [(torch.bfloat16, 13000, 4096), (torch.bfloat16, 1300, 40008), (torch.float32, 9000, 4096)])
+@pytest.mark.parametrize("dtype,N,H", [(torch.bfloat16, 13000, 4096), (torch.bfloat16, 1300, 40008), (torch.float32, 9000, 4096),
+                                       (torch.float32, 17000, 4104)])
 def test_rows_past_the_caches(B, dtype, fmt, N, H):
-    """Arrays of more than 96 MiB, against calls of fewer rows, whose blocks are the same."""
+    """Arrays of more than 96 MiB, of more than 256 in fp32, against calls of fewer rows, whose blocks are the same."""
     x = torch.empty(N, H, device="cuda", dtype=dtype)
     x.copy_(torch.randn(N, H, generator=torch.Generator("cuda").manual_seed(N), device="cuda"))
     x[7, 5], x[N - 1, H - 1] = float("nan"), float("inf")
