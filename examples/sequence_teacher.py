@@ -35,7 +35,7 @@ class Body:
 
 def decode(body, head, first, beams, steps, length_power=0.6):
     """Sequences of `steps` tokens at most behind the tokens first [n]: the best of each by its score a token^length_power, tokens
-    [n, steps] and lengths [n] (behind the end: END)."""
+    [n, steps] and lengths [n] (behind the end: END; 0 where none of its beams could go on)."""
     n, dev = first.shape[0], first.device
     state = body.step(torch.zeros(n * beams, head.H, device=dev), first.repeat_interleave(beams))
     tokens = torch.full((n * beams, steps), END, dtype=torch.int32, device=dev)
@@ -44,7 +44,9 @@ def decode(body, head, first, beams, steps, length_power=0.6):
     finished = length = torch.zeros(n, beams, dtype=torch.int32, device=dev)
     carried = B.BeamStates([state, tokens], beams)        # in place: rows that stay are not touched
     for t in range(steps):
-        z = head.logits(state)
+        z, status = head.logits(state, row_status=True)
+        # a state that holds an inf or NaN has no logits, and its beam no continuations
+        score = score.masked_fill((status.view(n, beams) != 0) & (finished == 0), -torch.inf)
         best = B.adwin_opd_beam_select(z, score, beams, finished=finished, length=length, end=END, length_power=length_power)
         score, finished, length = best["score"], best["finished"], best["length"]
         carried.reorder(best["parent"])
